@@ -149,6 +149,7 @@ def prepare(case, seed):
         s["fmt"] = {MX4: dn.DN_MXFP4, MX8: dn.DN_MXFP8}[case.get("fmt", MX4)]
         if kind == "cache":
             s["table"] = torch.zeros(dn.mx_bytes(s["fmt"], case["slots"], case["cols"]), device=_dev(), dtype=torch.uint8)
+            s["ws"] = torch.empty(dn.ac_mx_store_bytes(case["rows"], case["slots"]), device=_dev(), dtype=torch.uint8)
             s["out"] = torch.empty(case["rows"], case["cols"], device=_dev())
         elif kind == "lookup":
             s["table"] = dn.mx_quantize(s["fmt"], i["emb"])
@@ -184,9 +185,8 @@ def prepare(case, seed):
 # ----------------------------------------------------------------------------- the plain form
 
 def _pow2(e):
-    """2^e exactly, for integer e in [-254, 254]."""
-    h = torch.div(e, 2, rounding_mode="floor")
-    return torch.ldexp(torch.ones_like(e, dtype=torch.float64), h) * torch.ldexp(torch.ones_like(e, dtype=torch.float64), e - h)
+    """2^e exactly (a power function may round), for integer e in [-1022, 1023]."""
+    return ((e.to(torch.int64) + 1023) << 52).view(torch.float64)
 
 
 def _encode(x, fmt):
@@ -212,10 +212,10 @@ def _encode(x, fmt):
             code = torch.where(m < 2, 2 * m, torch.where(m < 4, m + 2, m / 2 + 4))
         else:
             # the quantum: 2^(e - 3) in [2^e, 2^(e + 1)), that of the least exponent -6 below
-            ex = (torch.frexp(m.clamp(min=2.0 ** -6))[1] - 1).double()
-            m = torch.round(m / torch.exp2(ex - 3)) * torch.exp2(ex - 3)
-            ex = (torch.frexp(m.clamp(min=2.0 ** -6))[1] - 1).double()
-            code = (ex + 6) * 8 + m / torch.exp2(ex - 3)   # below 2^-6 the second term is under 8
+            ex = torch.frexp(m.clamp(min=2.0 ** -6))[1] - 1
+            m = torch.round(m * _pow2(3 - ex)) * _pow2(ex - 3)
+            ex = torch.frexp(m.clamp(min=2.0 ** -6))[1] - 1
+            code = (ex + 6) * 8 + m * _pow2(3 - ex)        # below 2^-6 the second term is under 8
         code = torch.where(s[:, :, None] < 255, code, torch.zeros_like(code))
         sign = torch.signbit(t).to(torch.uint8) * (8 if fmt == MX4 else 128)
         codes[a:a + step] = (code.to(torch.uint8) + sign).reshape(-1, blocks * BLOCK)
@@ -286,7 +286,7 @@ def _run_plain(s):
 def _run_own(s):
     case, i, dn = s["case"], s["in"], s["dn"]
     if case["kind"] == "cache":
-        dn.ac_mx_store(s["fmt"], i["x"], i["slots"], s["table"], case["slots"])
+        dn.ac_mx_store(s["fmt"], i["x"], i["slots"], s["table"], case["slots"], s["ws"])
         dn.ac_mx_fetch(s["fmt"], s["table"], case["slots"], i["idx"], s["out"])
         return s["out"]
     if case["kind"] == "lookup":
@@ -347,6 +347,7 @@ def _quantised(x, fmt):
         values = values[:127]                                             # the last would be 480
     bounds = torch.tensor(_bounds(values), device=x.device, dtype=torch.float64)
     grid = torch.tensor(values, device=x.device, dtype=torch.float64)
+    powers = torch.tensor([2.0 ** k for k in range(-150, 129)], device=x.device, dtype=torch.float64)
     r, c = x.shape
     out = torch.empty(r, c, device=x.device, dtype=torch.float64)
     pad = -c % BLOCK
@@ -354,11 +355,10 @@ def _quantised(x, fmt):
     for a in range(0, r, step):
         v = torch.nn.functional.pad(x[a:a + step].double(), (0, pad)).unflatten(1, (-1, BLOCK))
         top = v.abs().amax(2, keepdim=True)
-        log = torch.floor(torch.log2(torch.where(top > 0, top, 1.0)))
-        # log2 is rounded: put it right next to powers of two
-        log = torch.where(torch.exp2(log) > top, log - 1, torch.where(torch.exp2(log + 1) <= top, log + 1, log))
-        log = torch.where(top > 0, log, 0.0)
-        scale = torch.exp2((log - math.floor(math.log2(values[-1]))).clamp(min=-127.0))
+        # the exponent of the largest magnitude, by search among exact powers of two
+        log = torch.bucketize(top, powers, right=True) - 1 - 150
+        log = (log - math.floor(math.log2(values[-1]))).clamp(min=-127)
+        scale = powers[log + 150]
         n = torch.bucketize((v / scale).abs(), bounds, right=True)
         out[a:a + step] = (torch.sign(v) * grid[n] * scale).flatten(1)[:, :c]
     return out
