@@ -19,6 +19,9 @@
  *   ac_lookup_batch_k                  ac_lookup_batch + the approximation level K chosen from the similarity
  *   ac_lookup_batch_noalloc            ac_lookup_batch on a stream, results in device memory, no allocation
  *   ac_fetch_latent                    copy cached latent #idx into an fp32 latent buffer
+ *   dn_mx_*                            microscaled (4- and 8-bit) rows: sizes, quantisation and back
+ *   ac_mx_store / ac_mx_fetch          quantise cached states or embeddings as they are written, read them back
+ *   ac_mx_lookup                       the nearest-prompt search over embeddings held in microscaled rows
  *   dn_unet_eps                        one UNet evaluation + guidance (per-step check hook)
  *   dn_vae_*                           the latent decoder after the loop (Table 3's VAE Decoder)
  *   dn_op_*                            single-kernel entry points (kernel checks, timing)
@@ -64,7 +67,9 @@ typedef enum {
   DN_EUNSUPPORTED = -4  /* valid but not supported by the library as built (e.g. no gfx950 device) */
 } dn_status;
 
-typedef enum { DN_FP32 = 0, DN_BF16 = 1, DN_FP8 = 2 } dn_dtype;
+/* DN_MXFP4 and DN_MXFP8 are microscaled rows (see dn_mx_quantize); DN_FP16 is a source type of
+ * the calls that quantise rows. */
+typedef enum { DN_FP32 = 0, DN_BF16 = 1, DN_FP8 = 2, DN_MXFP4 = 3, DN_MXFP8 = 4, DN_FP16 = 5 } dn_dtype;
 typedef enum { DN_WEIGHTS_HOST = 0, DN_WEIGHTS_DEVICE = 1 } dn_weights_location;
 typedef enum { DN_BETA_LINEAR = 0, DN_BETA_SCALED_LINEAR = 1 } dn_beta_schedule;
 
@@ -91,6 +96,10 @@ typedef struct {
  *                fp32 scale per output row (row max / 448) and whose two inputs (the
  *                third LayerNorm's output, the GEGLU output) are E4M3 at scale 1
  *                (nearest even, saturating at 448), multiplied on the fp8 matrix cores.
+ *                DN_MXFP4: the same with the feed-forward's matrices and both its inputs in
+ *                microscaled 4-bit rows (dn_mx_quantize; the matrices along their input dimension),
+ *                multiplied on the fp4 matrix cores: a quarter of the bf16 weights' bytes, and the
+ *                coarser of the two quantized levels. Transformer widths must be multiples of 128.
  * batch          images B; the UNet runs on 2B rows (B unconditional, then B
  *                conditional) for classifier-free guidance.
  * latent_*       latent channels (<= 64) and spatial size; H and W must be
@@ -294,6 +303,67 @@ dn_status ac_fetch_latent(const uint16_t* cache_latents, int64_t n, int64_t nume
                           void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Microscaled (MX) rows: the OCP Microscaling formats with 32-element blocks (OCP Microscaling Formats
+ * (MX) Specification v1.0). A row of `cols` values has B = ceil(cols / 32) blocks; a block holds 32 codes,
+ * E2M1 (DN_MXFP4: magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6) or E4M3 (DN_MXFP8, largest 448), and one scale
+ * byte s that stands for 2^(s - 127):
+ *   s = max(floor(log2 max|x|) - e + 127, 0), e = 2 (E2M1) or 8 (E4M3); 0 for a block of zeros
+ *   code = round(x / 2^(s - 127)), nearest even, saturating; value = code 2^(s - 127).
+ * A block with an infinity or a NaN gets s = 255 and reads back as NaN. Magnitudes above 1.5 (E2M1) or 1.75
+ * (E4M3) times the power of two below the block's largest saturate: the specification's rule.
+ * An MX buffer of `rows` rows (device, 16-byte aligned, dn_mx_bytes bytes):
+ *   codes [rows][B * 16] (DN_MXFP4: value i of a row in bits 4 (i % 2) .. of byte i / 2) or
+ *   [rows][B * 32] (DN_MXFP8), zero past `cols`; then scales [rows][B]; then padding that is never
+ *   written (reads go a few bytes past the last scale).
+ * An MX buffer of n rows is also a cache of n slots: a latent table (cols = latent_c*H*W) or an
+ * embedding table (cols = dim). All calls below are asynchronous on `stream`, allocate nothing and
+ * keep no state, so calls on different buffers may overlap and be captured into graphs.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of an MX buffer of `rows` x `cols` values, 1 <= cols <= 2^31 - 32. */
+dn_status dn_mx_bytes(int32_t dtype, int64_t rows, int64_t cols, int64_t* bytes);
+
+/* Quantises rows x [rows][ldx] (x_dtype DN_FP32, DN_BF16 or DN_FP16; ldx >= cols elements apart) into the
+ * MX buffer q (not overlapping x). rows < 2^31. */
+dn_status dn_mx_quantize(int32_t dtype, int32_t x_dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols,
+                         void* q, void* stream);
+
+/* The values of an MX buffer: y fp32 [rows][ldy], ldy >= cols; nothing is written past `cols`. */
+dn_status dn_mx_dequantize(int32_t dtype, const void* q, int64_t rows, int64_t cols, float* y, int64_t ldy,
+                           void* stream);
+
+/* Cache write (Sec. 4.7; the slots of dn_denoise_capture in 17/64 (DN_MXFP4) or 33/64 (DN_MXFP8) of their
+ * bf16 bytes, or prompt embeddings): row j of x (as in dn_mx_quantize, `dim` values) is quantised into
+ * slot slots[j] (device int64 [n_rows]) of `table`, an MX buffer of n_slots rows. Other slots keep their
+ * contents. Slots outside [0, n_slots) are skipped; if a slot occurs more than once in a call, the last of
+ * its rows is stored. ws: device, ac_mx_store_bytes(n_rows, n_slots) bytes (0 for few rows: NULL), free
+ * when the call's work has finished; overlapping calls need workspaces of their own, and calls that write
+ * the same slot must not overlap. n_rows < 2^31. */
+dn_status ac_mx_store_bytes(int64_t n_rows, int64_t n_slots, int64_t* bytes);
+dn_status ac_mx_store(int32_t dtype, int32_t x_dtype, const void* x, int64_t ldx, int64_t n_rows,
+                      const int64_t* slots, void* table, int64_t n_slots, int64_t dim, void* ws, void* stream);
+
+/* Cache read: row j of out (fp32 [n_idx][ldo], ldo >= dim) <- the values of slot idx[j] (device int64
+ * [n_idx], e.g. the out_idx of ac_mx_lookup). A row whose index lies outside [0, n_slots) is left as it
+ * was (the caller starts that prompt from noise, K = 0). */
+dn_status ac_mx_fetch(int32_t dtype, const void* table, int64_t n_slots, int64_t dim, const int64_t* idx,
+                      int64_t n_idx, float* out, int64_t ldo, void* stream);
+
+/* Nearest cached prompt (the search of ac_lookup_batch) over embeddings held in an MX table of n rows of
+ * `dim` values: for each query of query_embs (device fp16 [nq][dim]) the first row of maximal cosine with
+ * the values the row's codes stand for; products and sums in fp32. out_idx device int64 [nq], -1 for a
+ * query that is zero or not finite (or if every row is zero or holds a NaN block: such rows are never
+ * retrieved); out_score device float [nq] or NULL (0 where the index is -1); levels (host, read during
+ * the call) and out_k (device int32 [nq]) are both given, or both NULL: the approximation level as in
+ * ac_lookup_batch_k. ws: device, 16-byte aligned, ac_mx_lookup_bytes bytes, contents arbitrary;
+ * overlapping calls need workspaces of their own. Any nq >= 1, n >= 1, 1 <= dim <= 16384; up to dim
+ * 1024 the table is read once per 64 queries. */
+dn_status ac_mx_lookup_bytes(int32_t nq, int64_t n, int32_t dim, int64_t* bytes);
+dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, const void* table, int64_t n,
+                       int32_t dim, const ac_k_table* levels, int64_t* out_idx, float* out_score, int32_t* out_k,
+                       void* ws, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Single-kernel entry points. They run exactly the kernels dn_denoise runs and
  * exist for element-wise checks at full size and for timing one kernel. A GEMM
  * whose tile plan splits K also runs the split-K reduction kernel; its partial
@@ -319,7 +389,11 @@ dn_status ac_fetch_latent(const uint16_t* cache_latents, int64_t n, int64_t nume
  *   E4M3 codes in the fragment order of the 32x32x64 fp8 matrix-core step (per 32 rows
  *   and 64-deep step, the lanes' 32-byte operands in 2 KB), code = round(w / scale_n),
  *   then N fp32 scales scale_n = max_k |w[n][k]| / 448 (1 for a zero row);
- *   dn_packed_weight_elems gives the total in bytes. */
+ *   dn_packed_weight_elems gives the total in bytes.
+ * DN_MXFP4: w is fp32 [N][K] (N % 32 == 0, K % 128 == 0), quantised as the rows of dn_mx_quantize;
+ *   `out` (16-byte aligned) receives N * K / 2 bytes of E2M1 codes in the operand order of the 32x32x64
+ *   matrix-core step (per 32 rows and 64-deep step the lanes' 16 bytes in 1 KB), then the scales (per 64
+ *   rows and 128 deep, four bytes a lane); dn_packed_weight_elems gives the total in bytes. */
 dn_status dn_packed_weight_elems(int32_t dtype, int32_t N, int32_t K, int64_t* elems);
 dn_status dn_pack_weight(int32_t dtype, const void* w, int32_t N, int32_t K, void* out, void* stream);
 
@@ -337,7 +411,12 @@ dn_status dn_pack_weight(int32_t dtype, const void* w, int32_t N, int32_t K, voi
  * DN_FP8: x E4M3 codes [M][K], w packed for DN_FP8 (K % 128 == 0; GEGLU value / gate
  *   rows interleaved as above before packing), accumulator column n scaled by scale_n;
  *   y fp32 when y_f32 != 0, else E4M3 codes when geglu != 0 (the input of the next fp8
- *   layer), else bf16; resid fp32 or bf16 per resid_f32. */
+ *   layer), else bf16; resid fp32 or bf16 per resid_f32.
+ * DN_MXFP4: x an MX buffer (dn_mx_quantize) of M rows of K values, w packed for DN_MXFP4 (K % 128 == 0,
+ *   N % 32 == 0; GEGLU rows interleaved as above before packing); y fp32 when y_f32 != 0, else for
+ *   geglu != 0 an MX buffer of M rows of N values (the input of the next layer), else bf16; resid fp32 or
+ *   bf16 per resid_f32. A NaN block of x or w makes the outputs it enters NaN. No workspace. x, w and an MX output
+ *   16-byte aligned; other buffers aligned to their elements. */
 dn_status dn_op_linear(int32_t dtype, const void* x, const void* w, const float* bias, const void* resid,
                        int32_t resid_f32, void* y, int32_t y_f32, int64_t M, int32_t N, int32_t K, int32_t geglu,
                        void* stream);
@@ -389,8 +468,8 @@ dn_status dn_op_groupnorm(int32_t dtype, const void* x, void* y, int32_t n, int3
                           const float* gamma, const float* beta, float eps, int32_t silu, void* stream);
 
 /* LayerNorm over the last axis: x fp32 [M][C] (the residual stream), y [M][C]
- * in `dtype` (E4M3 codes for DN_FP8, nearest even, saturating); C a multiple of 4, at
- * most 2048. Asynchronous. */
+ * in `dtype` (E4M3 codes for DN_FP8, nearest even, saturating; an MX buffer of M rows of C
+ * values for DN_MXFP4, C % 32 == 0); C a multiple of 4, at most 2048. Asynchronous. */
 dn_status dn_op_layernorm(int32_t dtype, const float* x, void* y, int64_t M, int32_t C, const float* gamma,
                           const float* beta, float eps, void* stream);
 

@@ -190,6 +190,38 @@ void lookup_batch_host(const uint16_t* query_embs, int32_t nq, const uint16_t* c
 
 bool is_dtype(int32_t d) { return d == DN_FP32 || d == DN_BF16; }
 bool is_dtype8(int32_t d) { return is_dtype(d) || d == DN_FP8; }
+bool is_mx(int32_t d) { return d == DN_MXFP4 || d == DN_MXFP8; }
+bool is_dtype_op(int32_t d) { return is_dtype8(d) || d == DN_MXFP4; }  // operand types of the dense layers and LayerNorm
+static_assert(DN_MXFP4 == dn::kMx4 && DN_MXFP8 == dn::kMx8, "the kernels' format numbers");
+
+// Arguments the MX row calls share: a table of n_slots rows of `cols` values, `rows` rows in fp32 / bf16 /
+// fp16 (dense rows ld apart) on the other side.
+void check_mx(const char* who, int32_t dtype, const void* table, int64_t n_slots, int64_t cols, const void* x, int64_t ld,
+              int64_t rows) {
+  const std::string w(who);
+  DN_CHECK(is_mx(dtype), w + ": dtype must be DN_MXFP4 or DN_MXFP8");
+  DN_CHECK(table && x, w + ": null pointer");
+  DN_CHECK(n_slots >= 1 && cols >= 1 && rows >= 1 && rows <= 0x7fffffffll, w + ": bad sizes");
+  (void)dn::mx_bytes(dtype, n_slots, cols);
+  DN_CHECK(ld >= cols && ld <= (1ll << 40), w + ": row stride smaller than the row");
+  DN_CHECK(reinterpret_cast<uintptr_t>(table) % 16 == 0, w + ": the MX buffer must be 16-byte aligned");
+}
+
+void store_rows(const char* who, int32_t dtype, int32_t src, const void* x, int64_t ldx, int64_t rows, int64_t cols,
+                const int64_t* slots, int64_t n_slots, void* table, void* ws, void* stream) {
+  const std::string w(who);
+  DN_CHECK(src == DN_FP32 || src == DN_BF16 || src == DN_FP16, w + ": source dtype must be DN_FP32, DN_BF16 or DN_FP16");
+  DN_CHECK(reinterpret_cast<uintptr_t>(x) % (src == DN_FP32 ? 4 : 2) == 0, w + ": misaligned source");
+  const long long* sl = reinterpret_cast<const long long*>(slots);
+  int* owner = static_cast<int*>(ws);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (src == DN_FP32)
+    dn::mx_store<float>(dtype, static_cast<const float*>(x), ldx, rows, cols, sl, n_slots, table, owner, s);
+  else if (src == DN_BF16)
+    dn::mx_store<dn::bf16>(dtype, static_cast<const dn::bf16*>(x), ldx, rows, cols, sl, n_slots, table, owner, s);
+  else
+    dn::mx_store<_Float16>(dtype, static_cast<const _Float16*>(x), ldx, rows, cols, sl, n_slots, table, owner, s);
+}
 
 // Per-device state of the single-kernel GEMM entry points: CU count (tile
 // planning) and a zero block for implicit-conv padding reads.
@@ -424,14 +456,92 @@ dn_status ac_fetch_latent(const uint16_t* cache_latents, int64_t n, int64_t nume
   });
 }
 
+dn_status dn_mx_bytes(int32_t dtype, int64_t rows, int64_t cols, int64_t* bytes) {
+  return guarded([&] {
+    DN_CHECK(is_mx(dtype), "dn_mx_bytes: dtype must be DN_MXFP4 or DN_MXFP8");
+    DN_CHECK(bytes, "dn_mx_bytes: null pointer");
+    *bytes = dn::mx_bytes(dtype, rows, cols);
+  });
+}
+
+dn_status dn_mx_quantize(int32_t dtype, int32_t x_dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols, void* q,
+                         void* stream) {
+  return guarded([&] {
+    check_mx("dn_mx_quantize", dtype, q, rows, cols, x, ldx, rows);
+    store_rows("dn_mx_quantize", dtype, x_dtype, x, ldx, rows, cols, nullptr, rows, q, nullptr, stream);
+  });
+}
+
+dn_status dn_mx_dequantize(int32_t dtype, const void* q, int64_t rows, int64_t cols, float* y, int64_t ldy, void* stream) {
+  return guarded([&] {
+    check_mx("dn_mx_dequantize", dtype, q, rows, cols, y, ldy, rows);
+    dn::mx_fetch(dtype, q, rows, cols, nullptr, rows, y, ldy, as_stream(stream));
+  });
+}
+
+dn_status ac_mx_store_bytes(int64_t n_rows, int64_t n_slots, int64_t* bytes) {
+  return guarded([&] {
+    DN_CHECK(bytes, "ac_mx_store_bytes: null pointer");
+    DN_CHECK(n_rows >= 1 && n_slots >= 1, "ac_mx_store_bytes: bad sizes");
+    *bytes = static_cast<int64_t>(dn::mx_store_workspace(n_rows, n_slots));
+  });
+}
+
+dn_status ac_mx_store(int32_t dtype, int32_t x_dtype, const void* x, int64_t ldx, int64_t n_rows, const int64_t* slots,
+                      void* table, int64_t n_slots, int64_t dim, void* ws, void* stream) {
+  return guarded([&] {
+    check_mx("ac_mx_store", dtype, table, n_slots, dim, x, ldx, n_rows);
+    DN_CHECK(slots, "ac_mx_store: null slots");
+    DN_CHECK((ws && reinterpret_cast<uintptr_t>(ws) % 4 == 0) || dn::mx_store_workspace(n_rows, n_slots) == 0,
+             "ac_mx_store: this many rows need the workspace of ac_mx_store_bytes");
+    store_rows("ac_mx_store", dtype, x_dtype, x, ldx, n_rows, dim, slots, n_slots, table, ws, stream);
+  });
+}
+
+dn_status ac_mx_fetch(int32_t dtype, const void* table, int64_t n_slots, int64_t dim, const int64_t* idx, int64_t n_idx,
+                      float* out, int64_t ldo, void* stream) {
+  return guarded([&] {
+    check_mx("ac_mx_fetch", dtype, table, n_slots, dim, out, ldo, n_idx);
+    DN_CHECK(idx, "ac_mx_fetch: null indices");
+    dn::mx_fetch(dtype, table, n_slots, dim, reinterpret_cast<const long long*>(idx), n_idx, out, ldo, as_stream(stream));
+  });
+}
+
+dn_status ac_mx_lookup_bytes(int32_t nq, int64_t n, int32_t dim, int64_t* bytes) {
+  return guarded([&] {
+    DN_CHECK(bytes, "ac_mx_lookup_bytes: null pointer");
+    DN_CHECK(nq >= 1 && n >= 1 && dim >= 1, "ac_mx_lookup_bytes: bad sizes");
+    *bytes = static_cast<int64_t>(dn::mx_lookup_workspace());
+  });
+}
+
+dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, const void* table, int64_t n, int32_t dim,
+                       const ac_k_table* levels, int64_t* out_idx, float* out_score, int32_t* out_k, void* ws, void* stream) {
+  return guarded([&] {
+    check_mx("ac_mx_lookup", dtype, table, n, dim, query_embs, dim, nq);
+    DN_CHECK(out_idx && ws, "ac_mx_lookup: null pointer");
+    DN_CHECK((levels != nullptr) == (out_k != nullptr), "ac_mx_lookup: a level table and a level output go together");
+    DN_CHECK(reinterpret_cast<uintptr_t>(ws) % 16 == 0, "ac_mx_lookup: the workspace must be 16-byte aligned");
+    dn::KTable kt;
+    if (levels) kt = k_table(levels);
+    dn::mx_lookup(dtype, query_embs, nq, table, n, dim, ws, reinterpret_cast<long long*>(out_idx), out_score,
+                  levels ? &kt : nullptr, out_k, as_stream(stream));
+  });
+}
+
 dn_status dn_packed_weight_elems(int32_t dtype, int32_t N, int32_t K, int64_t* elems) {
   return guarded([&] {
-    DN_CHECK(is_dtype8(dtype), "dn_packed_weight_elems: bad dtype");
+    DN_CHECK(is_dtype_op(dtype), "dn_packed_weight_elems: bad dtype");
     DN_CHECK(elems, "dn_packed_weight_elems: null pointer");
     DN_CHECK(N >= 1 && K >= 1, "dn_packed_weight_elems: bad sizes");
     if (dtype == DN_FP8) {
       DN_CHECK(dn::gemm_fp8_layout(N, K), "dn_packed_weight_elems: DN_FP8 needs N % 32 == 0, K % 128 == 0");
       *elems = (int64_t)dn::gemm_fp8_code_bytes(N, K) + 4ll * N;
+      return;
+    }
+    if (dtype == DN_MXFP4) {
+      DN_CHECK(dn::gemm_mx4_layout(N, K), "dn_packed_weight_elems: DN_MXFP4 needs N % 32 == 0, K % 128 == 0");
+      *elems = (int64_t)dn::gemm_mx4_bytes(N, K);
       return;
     }
     *elems = dtype == DN_BF16 && dn::gemm_frag_layout(N, K) ? (int64_t)dn::gemm_frag_elems(N, K) : (int64_t)N * K;
@@ -440,8 +550,20 @@ dn_status dn_packed_weight_elems(int32_t dtype, int32_t N, int32_t K, int64_t* e
 
 dn_status dn_pack_weight(int32_t dtype, const void* w, int32_t N, int32_t K, void* out, void* stream) {
   return guarded([&] {
-    DN_CHECK(is_dtype8(dtype), "dn_pack_weight: bad dtype");
+    DN_CHECK(is_dtype_op(dtype), "dn_pack_weight: bad dtype");
     DN_CHECK(w && out, "dn_pack_weight: null pointer");
+    if (dtype == DN_MXFP4) {
+      DN_CHECK(dn::gemm_mx4_layout(N, K), "dn_pack_weight: DN_MXFP4 needs N % 32 == 0, K % 128 == 0");
+      DN_CHECK(reinterpret_cast<uintptr_t>(out) % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 4 == 0,
+               "dn_pack_weight: DN_MXFP4 needs a 16-byte aligned output and a 4-byte aligned source");
+      dn::PackParams p;
+      p.dst = out;
+      p.rows = p.src_rows = N;
+      p.cols = p.src_cols = K;
+      p.src = static_cast<const float*>(w);
+      dn::pack_mx4(p, static_cast<unsigned char*>(out) + dn::gemm_mx4_code_bytes(N, K), as_stream(stream));
+      return;
+    }
     if (dtype == DN_FP8) {
       DN_CHECK(dn::gemm_fp8_layout(N, K), "dn_pack_weight: DN_FP8 needs N % 32 == 0, K % 128 == 0");
       dn::PackParams p;
@@ -470,11 +592,30 @@ dn_status dn_op_linear(int32_t dtype, const void* x, const void* w, const float*
                        int32_t resid_f32, void* y, int32_t y_f32, int64_t M, int32_t N, int32_t K, int32_t geglu,
                        void* stream) {
   return guarded([&] {
-    DN_CHECK(is_dtype8(dtype), "dn_op_linear: bad dtype");
+    DN_CHECK(is_dtype_op(dtype), "dn_op_linear: bad dtype");
     DN_CHECK(x && w && y, "dn_op_linear: null pointer");
     DN_CHECK(M >= 1 && M <= 0x7fffffff && N >= 1 && K >= 1, "dn_op_linear: bad sizes");
     DN_CHECK(!geglu || N % 32 == 0, "dn_op_linear: GEGLU needs N % 32 == 0");
     DN_CHECK(!(geglu && resid), "dn_op_linear: GEGLU takes no residual");
+    if (dtype == DN_MXFP4) {
+      DN_CHECK(N <= 0x3fffffff && dn::gemm_mx4_layout(geglu ? 2 * N : N, K),
+               "dn_op_linear: DN_MXFP4 needs N % 32 == 0 and K % 128 == 0");
+      dn::GemmMx4Params q;
+      q.a = x;
+      q.b = w;
+      q.M = static_cast<int>(M);
+      q.N = geglu ? 2 * N : N;
+      q.K = K;
+      q.bias = bias;
+      q.resid = resid;
+      q.resid_f32 = resid_f32;
+      q.out = y;
+      q.out_f32 = y_f32;
+      q.geglu = geglu;
+      dn::gemm_mx4_check(q);
+      dn::gemm_mx4(q, current_cus(), as_stream(stream));
+      return;
+    }
     dn::GemmParams p;
     p.a0 = x;
     p.c0 = K;
@@ -666,9 +807,11 @@ dn_status dn_op_groupnorm(int32_t dtype, const void* x, void* y, int32_t n, int3
 dn_status dn_op_layernorm(int32_t dtype, const float* x, void* y, int64_t M, int32_t C, const float* gamma,
                           const float* beta, float eps, void* stream) {
   return guarded([&] {
-    DN_CHECK(is_dtype8(dtype), "dn_op_layernorm: bad dtype");
+    DN_CHECK(is_dtype_op(dtype), "dn_op_layernorm: bad dtype");
     DN_CHECK(x && y && gamma && beta, "dn_op_layernorm: null pointer");
-    if (dtype == DN_FP8)
+    if (dtype == DN_MXFP4)
+      dn::layernorm<dn::Mx4Row>(x, static_cast<dn::Mx4Row*>(y), M, C, gamma, beta, eps, as_stream(stream));
+    else if (dtype == DN_FP8)
       dn::layernorm<uint8_t>(x, static_cast<uint8_t*>(y), M, C, gamma, beta, eps, as_stream(stream));
     else if (dtype == DN_BF16)
       dn::layernorm<dn::bf16>(x, static_cast<dn::bf16*>(y), M, C, gamma, beta, eps, as_stream(stream));

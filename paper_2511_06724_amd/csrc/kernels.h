@@ -131,6 +131,10 @@ struct GroupNormParams {
 size_t groupnorm_workspace_floats(int n, int HW, int C, int G);
 template <typename T> void groupnorm(const GroupNormParams& p, hipStream_t s);
 
+// T = Mx4Row: the output is an MX4 buffer (C % 32 == 0).
+struct Mx4Row {
+  uint8_t byte;
+};
 template <typename T>
 void layernorm(const float* x, T* y, long long M, int C, const float* gamma, const float* beta, float eps,
                hipStream_t s);
@@ -173,6 +177,19 @@ struct PackParams {
   int Cin = 0, Cinp = 0;           // conv input channels and padded count
   int frag = 0;                    // 1: write dst in fragment order (gemm_frag.hip; ld_dst unused)
 };
+// Source row of packed row r (or -1 for a zero row).
+__device__ inline long long pack_src_row(const PackParams& p, int r) {
+  if (p.row_mode == 1) {  // GEGLU: 32-row blocks alternate value / gate
+    const int half = p.src_rows / 2;
+    const int blk = r / 64, w = r - blk * 64;
+    return w < 32 ? (long long)blk * 32 + w : (long long)half + blk * 32 + (w - 32);
+  }
+  if (p.row_mode == 2) {  // head padding: head h rows [h*Dp, h*Dp + D) <- source [h*D, h*D + D)
+    const int h = r / p.Dp, d = r - h * p.Dp;
+    return d < p.D ? (long long)h * p.D + d : -1;
+  }
+  return r < p.src_rows ? r : -1;
+}
 template <typename T> void pack(const PackParams& p, hipStream_t s);
 // E4M3 quantisation of a [rows][cols] fp32 source (the same row mapping as pack; column
 // mode 0 only): per destination row r, scale[r] = max_c |src| / 448 (1 for a zero row)
@@ -181,7 +198,48 @@ template <typename T> void pack(const PackParams& p, hipStream_t s);
 void pack_fp8(const PackParams& p, float* scales, hipStream_t s);
 void pack_bias(float* dst, int n, const float* src, int src_n, int row_mode, int D, int Dp, hipStream_t s);
 
+// ---------------------------------------------------------------- microscaled rows (mx.h)
+constexpr int kMx4 = 3, kMx8 = 4;  // DN_MXFP4, DN_MXFP8
+constexpr long long kMxMaxCols = (1ll << 31) - 32;
+// Bytes of a buffer of `rows` rows (checked), and where its scales begin.
+long long mx_bytes(int fmt, long long rows, long long cols);
+size_t mx_scale_offset(int fmt, long long rows, long long cols);
+// Quantises rows x [rows][ldx] into the slots of table [n_slots][cols]: row j into slots[j] (device;
+// entries outside [0, n_slots) are skipped, the last row of a slot wins), or into slot j without
+// slots. owner: mx_store_workspace() bytes, needed with slots.
+size_t mx_store_workspace(long long rows, long long n_slots);
+template <typename T>
+void mx_store(int fmt, const T* x, long long ldx, long long rows, long long cols, const long long* slots, long long n_slots,
+              void* table, int* owner, hipStream_t s);
+// Row j of y <- slot idx[j] (device; entries outside the table leave the row), or slot j without idx.
+void mx_fetch(int fmt, const void* table, long long n_slots, long long cols, const long long* idx, long long rows, float* y,
+              long long ldy, hipStream_t s);
+// 4-bit weights from a [rows][cols] fp32 source (the row mapping of pack): codes in operand order to
+// p.dst, scales to `scales` (gemm_mx4_code_bytes() further in a packed matrix).
+void pack_mx4(const PackParams& p, unsigned char* scales, hipStream_t s);
+
+// 4-bit product: C[m][n] = sum_k A[m][k] B[n][k], A an MX4 buffer of M rows, B packed by pack_mx4;
+// then + bias[n] + resid[m][n] to fp32 or bf16, or GEGLU (columns in value / gate block pairs) to fp32
+// or to an MX4 buffer of n_out = N / 2 columns. N % 32 == 0 (GEGLU: 64), K % 128 == 0.
+struct GemmMx4Params {
+  const void* a = nullptr;
+  const void* b = nullptr;
+  int M = 0, N = 0, K = 0;
+  const float* bias = nullptr;
+  const void* resid = nullptr;  // [M][N]
+  int resid_f32 = 0;
+  void* out = nullptr;
+  int out_f32 = 0;
+  int geglu = 0;
+};
+bool gemm_mx4_layout(int N, int K);
+size_t gemm_mx4_code_bytes(int N, int K);
+size_t gemm_mx4_bytes(int N, int K);  // codes and scales of a packed matrix
+void gemm_mx4_check(const GemmMx4Params& p);  // throws for what gemm_mx4 does not take
+void gemm_mx4(const GemmMx4Params& p, int cus, hipStream_t s);
+
 // ---------------------------------------------------------------- cache lookup
+constexpr int kMxLookupMaxDim = 16384;
 // Similarity-driven approximation level: a retrieved cosine s gets level[j],
 // j = #{i < n : s >= thr[i]} (fp32 comparisons); a query that retrieved nothing gets 0.
 constexpr int kMaxKLevels = 16;
@@ -207,5 +265,10 @@ bool lookup_batch_supported(const uint16_t* q, const uint16_t* cache, long long 
 void lookup_batch(const uint16_t* q, int nq, const uint16_t* cache, long long n, int dim, void* ws,
                   long long* idx_out, float* score_out, hipStream_t s, const KTable* kt = nullptr,
                   int* k_out = nullptr);
+// Top-1 rows of an MX table [n][dim] for any number of queries (mx_lookup.hip); outputs in device
+// memory (score_out, k_out may be null). ws: mx_lookup_workspace() bytes.
+size_t mx_lookup_workspace();
+void mx_lookup(int fmt, const uint16_t* q, int nq, const void* table, long long n, int dim, void* ws, long long* idx_out,
+               float* score_out, const KTable* kt, int* k_out, hipStream_t s);
 
 }  // namespace dn

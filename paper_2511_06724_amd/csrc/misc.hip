@@ -139,20 +139,6 @@ __global__ void bf16_to_f32_kernel(const uint16_t* src, float* dst, long long n)
     dst[i] = __uint_as_float(static_cast<uint32_t>(src[i]) << 16);
 }
 
-// Source row of packed row r (or -1 for a zero row).
-__device__ __forceinline__ long long pack_src_row(const PackParams& p, int r) {
-  if (p.row_mode == 1) {  // GEGLU: 32-row blocks alternate value / gate
-    const int half = p.src_rows / 2;
-    const int blk = r / 64, w = r - blk * 64;
-    return w < 32 ? (long long)blk * 32 + w : (long long)half + blk * 32 + (w - 32);
-  }
-  if (p.row_mode == 2) {  // head padding: head h rows [h*Dp, h*Dp + D) <- source [h*D, h*D + D)
-    const int h = r / p.Dp, d = r - h * p.Dp;
-    return d < p.D ? (long long)h * p.D + d : -1;
-  }
-  return r < p.src_rows ? r : -1;
-}
-
 template <typename T> __global__ void pack_kernel(PackParams p) {
   const long long total = (long long)p.rows * p.cols;
   for (long long i = blockIdx.x * (long long)blockDim.x + threadIdx.x; i < total;

@@ -146,8 +146,8 @@ struct TableBuilder {
 
 void validate_config(const dn_config& c) {
   DN_CHECK(c.abi_version == DN_ABI_VERSION, "config: abi_version mismatch");
-  DN_CHECK(c.dtype == DN_FP32 || c.dtype == DN_BF16 || c.dtype == DN_FP8,
-           "config: dtype must be DN_FP32, DN_BF16 or DN_FP8");
+  DN_CHECK(c.dtype == DN_FP32 || c.dtype == DN_BF16 || c.dtype == DN_FP8 || c.dtype == DN_MXFP4,
+           "config: dtype must be DN_FP32, DN_BF16, DN_FP8 or DN_MXFP4");
   DN_CHECK(c.batch >= 1 && c.batch <= 64, "config: batch must be in [1, 64]");
   DN_CHECK(c.latent_c >= 1 && c.latent_c <= kCinPad, "config: latent_c must be in [1, 64]");
   DN_CHECK(c.n_levels >= 1 && c.n_levels <= DN_MAX_LEVELS, "config: n_levels must be in [1, 4]");
@@ -177,8 +177,8 @@ void validate_config(const dn_config& c) {
     DN_CHECK(lv.channels % c.gn_groups == 0, "config: level channels not divisible by gn_groups");
     DN_CHECK(lv.depth >= 0 && lv.depth <= 64, "config: level depth must be in [0, 64]");
     const bool attn = lv.depth > 0 || (l == c.n_levels - 1 && c.mid_depth > 0);
-    if (c.dtype == DN_FP8 && (lv.depth > 0 || (l == c.n_levels - 1 && c.mid_depth > 0)))
-      DN_CHECK(lv.channels % 128 == 0, "config: DN_FP8 needs transformer widths that are multiples of 128");
+    if ((c.dtype == DN_FP8 || c.dtype == DN_MXFP4) && attn)
+      DN_CHECK(lv.channels % 128 == 0, "config: DN_FP8 and DN_MXFP4 need transformer widths that are multiples of 128");
     if (attn) {
       DN_CHECK(lv.heads >= 1 && lv.head_dim >= 1 && lv.head_dim <= 64, "config: heads >= 1, head_dim in [1, 64]");
       DN_CHECK(lv.heads * lv.head_dim == lv.channels, "config: heads * head_dim must equal channels");
@@ -259,6 +259,7 @@ struct LinW {
   void* w = nullptr;  // [n][k]
   float* b = nullptr;
   float* scale = nullptr;  // fp8 matrices: per-row scales (w then holds E4M3 codes)
+  bool mx4 = false;        // 4-bit matrices: packed codes and block scales in w
   int n = 0, k = 0;
 };
 struct Norm {
@@ -297,6 +298,7 @@ struct Model {
   size_t esz = 2;    // element size of activations / packed weights
   bool bf = true;
   bool fp8ff = false;  // the GEGLU feed-forward on E4M3 operands (dtype DN_FP8)
+  bool mx4ff = false;  // the same on microscaled E2M1 operands (dtype DN_MXFP4)
   int temb_dim = 0, temb_total = 0;
   // parameters
   void* packed = nullptr;  // all packed weight matrices
@@ -438,6 +440,26 @@ struct Packer {
     }
     return l;
   }
+  // 4-bit (MX) matrix: codes and block scales in operand order (no bias)
+  LinW lin_mx4(const std::string& n, int rows, int cols, int row_mode) {
+    LinW l;
+    l.n = rows;
+    l.k = cols;
+    l.mx4 = true;
+    l.w = alloc_packed((gemm_mx4_bytes(rows, cols) + m->esz - 1) / m->esz);
+    if (!dry) {
+      PackParams p;
+      p.dst = l.w;
+      p.rows = rows;
+      p.cols = cols;
+      p.src = blob + t(n + ".w").offset;
+      p.row_mode = row_mode;
+      p.src_rows = rows;
+      p.src_cols = cols;
+      pack_mx4(p, static_cast<unsigned char*>(l.w) + gemm_mx4_code_bytes(rows, cols), s);
+    }
+    return l;
+  }
 };
 
 void build(Model* m, Packer& pk, const dn_config& cfg, const std::vector<Walker::Ev>& ev) {
@@ -538,6 +560,8 @@ void build(Model* m, Packer& pk, const dn_config& cfg, const std::vector<Walker:
           tb.ff1.k = C;
           if (m->fp8ff) {
             tb.ff1 = pk.lin_fp8(b + ".ff1", 2 * F * C, C, 1);
+          } else if (m->mx4ff) {
+            tb.ff1 = pk.lin_mx4(b + ".ff1", 2 * F * C, C, 1);
           } else {
             tb.ff1.w = pk.alloc_packed((size_t)2 * F * C * C);
             pk.pack_mat(tb.ff1.w, 2 * F * C, C, C, pk.t(b + ".ff1.w"), 1, 0, 2 * F * C, C);
@@ -546,6 +570,9 @@ void build(Model* m, Packer& pk, const dn_config& cfg, const std::vector<Walker:
           if (!pk.dry) pack_bias(tb.ff1.b, 2 * F * C, pk.blob + pk.t(b + ".ff1.b").offset, 2 * F * C, 1, 0, 0, pk.s);
           if (m->fp8ff) {
             tb.ff2 = pk.lin_fp8(b + ".ff2", C, F * C, 0);
+            tb.ff2.b = pk.copy_param(b + ".ff2.b");
+          } else if (m->mx4ff) {
+            tb.ff2 = pk.lin_mx4(b + ".ff2", C, F * C, 0);
             tb.ff2.b = pk.copy_param(b + ".ff2.b");
           } else {
             tb.ff2 = pk.lin(b + ".ff2", C, F * C, true);
@@ -693,6 +720,7 @@ Model* model_create(const dn_config& cfg, const float* weights, size_t n_floats,
   m->n = 2 * cfg.batch;
   m->bf = cfg.dtype != DN_FP32;
   m->fp8ff = cfg.dtype == DN_FP8;
+  m->mx4ff = cfg.dtype == DN_MXFP4;
   m->esz = m->bf ? 2 : 4;
   m->temb_dim = 4 * cfg.model_channels;
   const auto ev = walk(cfg);
@@ -869,6 +897,22 @@ template <typename T> struct Exec {
   void linear(const LinW& w, const void* x, int ldx, long long M, void* out, int ldo, bool out_f32,
               const void* resid = nullptr, int ldr = 0, bool resid_f32 = false, bool geglu = false,
               const void* x1 = nullptr, int c0 = 0, int c1 = 0, const VtOut& vt = VtOut()) {
+    if (w.mx4) {  // x an MX4 buffer; the hidden layer (geglu) stays in one, everything is dense
+      GemmMx4Params q;
+      q.a = x;
+      q.b = w.w;
+      q.M = static_cast<int>(M);
+      q.N = w.n;
+      q.K = w.k;
+      q.bias = w.b;
+      q.resid = resid;
+      q.resid_f32 = resid_f32;
+      q.out = out;
+      q.out_f32 = out_f32;
+      q.geglu = geglu;
+      if (!dry) gemm_mx4(q, m->cus, s);
+      return;
+    }
     GemmParams p;
     p.a0 = x;
     p.a1 = x1;
@@ -969,6 +1013,10 @@ template <typename T> struct Exec {
     bool resid = true;
   };
   Pending residual_gemm(const LinW& w, const void* x, int ldx, long long M, bool resid) {
+    if (w.mx4) {
+      linear(w, x, ldx, M, m->R, w.n, true, resid ? m->R : nullptr, w.n, true);
+      return Pending{};
+    }
     const GemmPlan g = w.scale ? gemm_plan_fp8(static_cast<int>(M), w.n, w.k, 0, m->cus, true, true)
                                : gemm_plan<T>(static_cast<int>(M), w.n, w.k, 0, m->cus, false, true, false, true);
     if (!g.frag || g.split == 1) {
@@ -1004,9 +1052,17 @@ template <typename T> struct Exec {
     }
     return Pending{&w, g.split, resid};
   }
-  // fp8: the LayerNorm feeding the fp8 feed-forward writes E4M3 codes
-  void ln_after(const Pending& pd, long long M, int C, const Norm& nm, bool fp8 = false) {
+  // fp8: the LayerNorm feeding the fp8 feed-forward writes E4M3 codes; mx4: an MX4 buffer
+  void ln_after(const Pending& pd, long long M, int C, const Norm& nm, bool fp8 = false, bool mx4 = false) {
     if (dry) return;
+    if (mx4) {
+      if (pd.nsplit)
+        layernorm_reduce<Mx4Row>(m->R, P_<Mx4Row>(m->a), M, C, nm.g, nm.b, m->cfg.ln_eps, m->split_ws, pd.nsplit,
+                                 pd.w->b, pd.resid, s);
+      else
+        layernorm<Mx4Row>(m->R, P_<Mx4Row>(m->a), M, C, nm.g, nm.b, m->cfg.ln_eps, s);
+      return;
+    }
     if (fp8) {
       if (pd.nsplit)
         layernorm_reduce<uint8_t>(m->R, P_<uint8_t>(m->a), M, C, nm.g, nm.b, m->cfg.ln_eps, m->split_ws, pd.nsplit,
@@ -1053,7 +1109,7 @@ template <typename T> struct Exec {
       attention_(m->q2, P, (long long)HW * P, kv, P, (long long)m->cfg.ctx_len * P, vtc,
                  (m->cfg.ctx_len + 63) / 64 * 64, HW, m->cfg.ctx_len, x);
       pd = residual_gemm(b.o2, m->o, P, M, true);
-      ln_after(pd, M, C, b.ln3, m->fp8ff);
+      ln_after(pd, M, C, b.ln3, m->fp8ff, m->mx4ff);
       linear(b.ff1, m->a, C, M, m->ff, m->cfg.ff_mult * C, false, nullptr, 0, false, true);
       if (!last)
         pd = residual_gemm(b.ff2, m->ff, m->cfg.ff_mult * C, M, true);

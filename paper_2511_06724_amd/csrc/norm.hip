@@ -19,7 +19,9 @@
 //
 // LayerNorm: one wave per token row in registers, two-pass mean / variance,
 // 16-byte loads and 8-byte (bf16) stores.
-#include "kernels.h"
+#include <type_traits>
+
+#include "mx.h"
 
 namespace dn {
 namespace {
@@ -495,10 +497,20 @@ template <> struct Store4<float> {
 // use, so a row waits on one memory latency; the two wave sums use DPP lane moves;
 // vector columns past C are skipped wave-uniformly, lanes past C read a valid column and
 // are masked.
+// Four values of a row of an MX4 buffer [M][C], lanes of eight a block: y the row's codes, sc its scales.
+__device__ __forceinline__ void st4_mx(uint8_t* y, uint8_t* sc, int i, float a, float b, float c, float d) {
+  const float v[8] = {a, b, c, d, 0.f, 0.f, 0.f, 0.f};
+  const unsigned s = mx_scale<kMx4>(oct_umax(max(max(mx_abs_bits(a), mx_abs_bits(b)), max(mx_abs_bits(c), mx_abs_bits(d)))));
+  *reinterpret_cast<unsigned short*>(y + 2 * i) = static_cast<unsigned short>(mx4_codes8(v, s));
+  if ((i & 7) == 0) sc[i / 8] = static_cast<uint8_t>(s);
+}
+
+// T = Mx4Row: y is an MX4 buffer (C % 32 == 0, so the eight lanes of a block are active together).
 template <typename T, int NS>
 __global__ __launch_bounds__(256) void ln_kernel(float* x, T* y, long long M, int C, const float* gamma,
                                                  const float* beta, float eps, const float* part, long long slab,
                                                  const float* bias, int resid) {
+  constexpr bool kMx = std::is_same<T, Mx4Row>::value;
   const int lane = threadIdx.x & 63;
   const long long row = blockIdx.x * 4ll + (threadIdx.x >> 6);
   if (row >= M) return;
@@ -571,7 +583,9 @@ __global__ __launch_bounds__(256) void ln_kernel(float* x, T* y, long long M, in
     }
   }
   const float rstd = rsqrtf(wave_sum_dpp(q) / C + eps);
-  T* yr = y + row * C;
+  T* yr = y + (kMx ? 0 : row * C);
+  uint8_t* const mc = reinterpret_cast<uint8_t*>(y) + row * (C / 2);                 // MX4: the row's codes
+  uint8_t* const ms = reinterpret_cast<uint8_t*>(y) + M * (C / 2) + row * (C / 32);  // and scales
 #pragma unroll
   for (int j = 0; j < kLnMaxVec; ++j) {
     const int i = lane + 64 * j;
@@ -584,8 +598,12 @@ __global__ __launch_bounds__(256) void ln_kernel(float* x, T* y, long long M, in
         g = g4[i];
         bb = b4[i];
       }
-      Store4<T>::st(yr + 4 * i, (v[j].x - mean) * rstd * g.x + bb.x, (v[j].y - mean) * rstd * g.y + bb.y,
-                    (v[j].z - mean) * rstd * g.z + bb.z, (v[j].w - mean) * rstd * g.w + bb.w);
+      const float o0 = (v[j].x - mean) * rstd * g.x + bb.x, o1 = (v[j].y - mean) * rstd * g.y + bb.y;
+      const float o2 = (v[j].z - mean) * rstd * g.z + bb.z, o3 = (v[j].w - mean) * rstd * g.w + bb.w;
+      if constexpr (kMx)
+        st4_mx(mc, ms, i, o0, o1, o2, o3);
+      else
+        Store4<T>::st(yr + 4 * i, o0, o1, o2, o3);
     }
   }
 }
@@ -652,8 +670,9 @@ void layernorm_reduce(float* x, T* y, long long M, int C, const float* gamma, co
   DN_CHECK(M >= 1 && C >= 4 && C % 4 == 0 && C <= 4 * 64 * kLnMaxVec, "layernorm: C must be a multiple of 4, <= 2048");
   DN_CHECK(x && y && gamma && beta, "layernorm: null");
   DN_CHECK(((uintptr_t)x | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)part | (uintptr_t)bias) % 16 == 0 &&
-               (uintptr_t)y % (4 * sizeof(T)) == 0,
-           "layernorm: x, gamma, beta, partials and bias must be 16-byte aligned, y aligned to 4 elements");
+               (uintptr_t)y % (std::is_same<T, Mx4Row>::value ? 16 : 4 * sizeof(T)) == 0,
+           "layernorm: x, gamma, beta, partials and bias must be 16-byte aligned, y aligned to 4 elements (MX: 16 bytes)");
+  DN_CHECK((!std::is_same<T, Mx4Row>::value) || C % kMxBlock == 0, "layernorm: an MX output needs C % 32 == 0");
   DN_CHECK(nsplit == 0 || part, "layernorm: partial slabs missing");
   switch (nsplit) {
     case 0: launch_ln<T, 0>(x, y, M, C, gamma, beta, eps, part, bias, resid, s); break;
@@ -680,6 +699,9 @@ template void layernorm_reduce<bf16>(float*, bf16*, long long, int, const float*
                                      int, const float*, bool, hipStream_t);
 template void layernorm_reduce<uint8_t>(float*, uint8_t*, long long, int, const float*, const float*, float,
                                         const float*, int, const float*, bool, hipStream_t);
+template void layernorm_reduce<Mx4Row>(float*, Mx4Row*, long long, int, const float*, const float*, float, const float*,
+                                       int, const float*, bool, hipStream_t);
+template void layernorm<Mx4Row>(const float*, Mx4Row*, long long, int, const float*, const float*, float, hipStream_t);
 template void layernorm<uint8_t>(const float*, uint8_t*, long long, int, const float*, const float*, float,
                                  hipStream_t);
 

@@ -16,7 +16,7 @@ from .workloads import DnConfig, VaeConfig
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libargus_dn.so")
 
 DN_OK, DN_EINVAL, DN_ENOMEM, DN_EHIP, DN_EUNSUPPORTED = 0, -1, -2, -3, -4
-DN_FP32, DN_BF16, DN_FP8 = 0, 1, 2
+DN_FP32, DN_BF16, DN_FP8, DN_MXFP4, DN_MXFP8, DN_FP16 = 0, 1, 2, 3, 4, 5
 DN_WEIGHTS_HOST, DN_WEIGHTS_DEVICE = 0, 1
 ABI_VERSION = 1
 MAX_LEVELS = 4
@@ -26,7 +26,8 @@ EXPORTED = ("dn_weight_count", "dn_weight_table", "dn_create", "dn_denoise", "dn
             "dn_op_attention", "dn_op_groupnorm", "dn_op_layernorm", "dn_op_layernorm_slabs", "dn_op_linear_vt",
             "dn_probe_mfma_rate",
             "dn_destroy", "dn_last_error", "dn_vae_weight_count", "dn_vae_weight_table", "dn_vae_create",
-            "dn_vae_decode", "dn_vae_destroy", "argus_oda", "argus_route", "argus_select_worker", "argus_last_error")
+            "dn_vae_decode", "dn_vae_destroy", "dn_mx_bytes", "dn_mx_quantize", "dn_mx_dequantize", "ac_mx_store_bytes",
+            "ac_mx_store", "ac_mx_fetch", "ac_mx_lookup_bytes", "ac_mx_lookup", "argus_oda", "argus_route", "argus_select_worker", "argus_last_error")
 
 
 AC_MAX_K_LEVELS = 16
@@ -91,6 +92,14 @@ def _load():
         "ac_lookup_batch_k": [P, I32, P, I64, I32, C.POINTER(_KTable), P, P, P],
         "ac_lookup_batch_noalloc": [P, I32, P, I64, I32, P, P, P],
         "ac_fetch_latent": [P, I64, I64, I64, P, P],
+        "dn_mx_bytes": [I32, I64, I64, C.POINTER(I64)],
+        "dn_mx_quantize": [I32, I32, P, I64, I64, I64, P, P],
+        "dn_mx_dequantize": [I32, P, I64, I64, P, I64, P],
+        "ac_mx_store_bytes": [I64, I64, C.POINTER(I64)],
+        "ac_mx_store": [I32, I32, P, I64, I64, P, P, I64, I64, P, P],
+        "ac_mx_fetch": [I32, P, I64, I64, P, I64, P, I64, P],
+        "ac_mx_lookup_bytes": [I32, I64, I32, C.POINTER(I64)],
+        "ac_mx_lookup": [I32, P, I32, P, I64, I32, C.POINTER(_KTable), P, P, P, P, P],
         "dn_packed_weight_elems": [I32, I32, I32, C.POINTER(I64)],
         "dn_pack_weight": [I32, P, I32, I32, P, P],
         "dn_op_linear": [I32, P, P, P, P, I32, P, I32, I64, I32, I32, I32, P],
@@ -364,6 +373,126 @@ def ac_fetch_latent(cache_latents, idx, latent, stream=None):
     _check(lib.ac_fetch_latent(_ptr(cache_latents), n, numel, idx, _ptr(latent), _stream(stream)))
 
 
+# ----------------------------------------------------------------------------- microscaled rows
+
+def mx_bytes(dtype, rows, cols):
+    """Bytes of an MX buffer (DN_MXFP4 or DN_MXFP8) of `rows` rows of `cols` values."""
+    n = C.c_int64()
+    _check(lib.dn_mx_bytes(dtype, rows, cols, C.byref(n)))
+    return n.value
+
+
+def _rows(x, name):
+    """(dtype, row stride, rows, columns) of a row source: a 2-D tensor whose rows are dense."""
+    import torch
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name}: a 2-D tensor with dense rows is needed")
+    dt = {torch.float32: DN_FP32, torch.bfloat16: DN_BF16, torch.float16: DN_FP16}.get(x.dtype)
+    if dt is None:
+        raise ValueError(f"{name}: rows must be float32, bfloat16 or float16")
+    return dt, max(x.stride(0), x.shape[1]) if x.shape[0] == 1 else x.stride(0), x.shape[0], x.shape[1]
+
+
+def _buffer(t, need, name):
+    """Checks a caller's byte buffer (uint8, dense) against the bytes a call accesses."""
+    if t.numel() * t.element_size() < need or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous buffer of at least {need} bytes is needed")
+
+
+def _index(t, name):
+    import torch
+    if t.dtype != torch.int64 or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{name}: a dense 1-D int64 tensor is needed")
+
+
+def mx_quantize(dtype, x, q=None, stream=None):
+    """Rows x [rows, cols] (float32, bfloat16 or float16, any row stride) -> an MX buffer (uint8
+    tensor of mx_bytes bytes; `q` or a new one)."""
+    import torch
+    xt, ldx, rows, cols = _rows(x, "mx_quantize")
+    need = mx_bytes(dtype, rows, cols)
+    if q is None:
+        q = torch.empty(need, device=x.device, dtype=torch.uint8)
+    _buffer(q, need, "mx_quantize")
+    _check(lib.dn_mx_quantize(dtype, xt, _ptr(x), ldx, rows, cols, _ptr(q), _stream(stream)))
+    return q
+
+
+def mx_dequantize(dtype, q, rows, cols, y=None, stream=None):
+    """The fp32 values [rows, cols] an MX buffer stands for (into `y` or a new tensor)."""
+    import torch
+    _buffer(q, mx_bytes(dtype, rows, cols), "mx_dequantize")
+    if y is None:
+        y = torch.empty(rows, cols, device=q.device)
+    yt, ldy, r, c = _rows(y, "mx_dequantize")
+    if yt != DN_FP32 or (r, c) != (rows, cols):
+        raise ValueError("mx_dequantize: y must be float32 [rows, cols]")
+    _check(lib.dn_mx_dequantize(dtype, _ptr(q), rows, cols, _ptr(y), ldy, _stream(stream)))
+    return y
+
+
+def ac_mx_store_bytes(n_rows, n_slots):
+    """Workspace bytes of ac_mx_store (0: none is needed)."""
+    n = C.c_int64()
+    _check(lib.ac_mx_store_bytes(n_rows, n_slots, C.byref(n)))
+    return n.value
+
+
+def ac_mx_store(dtype, x, slots, table, n_slots, ws=None, stream=None):
+    """Quantises row j of x [n, dim] into slot slots[j] (int64 CUDA tensor [n]) of an MX table of
+    n_slots slots (uint8, mx_bytes(dtype, n_slots, dim)); ws: uint8, ac_mx_store_bytes(n, n_slots)."""
+    xt, ldx, n, dim = _rows(x, "ac_mx_store")
+    _index(slots, "ac_mx_store")
+    if slots.shape[0] != n:
+        raise ValueError("ac_mx_store: one slot per row is needed")
+    _buffer(table, mx_bytes(dtype, n_slots, dim), "ac_mx_store")
+    need = ac_mx_store_bytes(n, n_slots)
+    if ws is not None:
+        _buffer(ws, need, "ac_mx_store workspace")
+    _check(lib.ac_mx_store(dtype, xt, _ptr(x), ldx, n, _ptr(slots), _ptr(table), n_slots, dim,
+                           _ptr(ws) if need else None, _stream(stream)))
+
+
+def ac_mx_fetch(dtype, table, n_slots, idx, out, stream=None):
+    """Row j of out [n, dim] (float32) <- slot idx[j] (int64 CUDA tensor [n]) of an MX table; rows whose
+    index lies outside the table (the -1 of a lookup) are left as they are."""
+    ot, ldo, n, dim = _rows(out, "ac_mx_fetch")
+    _index(idx, "ac_mx_fetch")
+    if ot != DN_FP32 or idx.shape[0] != n:
+        raise ValueError("ac_mx_fetch: out must be float32 with one row per index")
+    _buffer(table, mx_bytes(dtype, n_slots, dim), "ac_mx_fetch")
+    _check(lib.ac_mx_fetch(dtype, _ptr(table), n_slots, dim, _ptr(idx), n, _ptr(out), ldo, _stream(stream)))
+
+
+def ac_mx_lookup_bytes(nq, n, dim):
+    """Workspace bytes of ac_mx_lookup."""
+    b = C.c_int64()
+    _check(lib.ac_mx_lookup_bytes(nq, n, dim, C.byref(b)))
+    return b.value
+
+
+def ac_mx_lookup(dtype, queries, table, n, ws, out_idx, out_score=None, out_k=None, thresholds=None, levels=None,
+                 stream=None):
+    """The nearest row of an MX table of n embeddings for every query [nq, dim] (float16, dense): out_idx
+    int64, out_score float32 or None, and with a threshold table out_k int32 (CUDA tensors [nq])."""
+    qt, ldq, nq, dim = _rows(queries, "ac_mx_lookup")
+    if qt != DN_FP16 or ldq != dim:
+        raise ValueError("ac_mx_lookup: queries must be dense float16 rows")
+    _buffer(table, mx_bytes(dtype, n, dim), "ac_mx_lookup")
+    _buffer(ws, ac_mx_lookup_bytes(nq, n, dim), "ac_mx_lookup workspace")
+    _index(out_idx, "ac_mx_lookup")
+    for t, size, name in ((out_idx, 8, "out_idx"), (out_score, 4, "out_score"), (out_k, 4, "out_k")):
+        if t is not None and (t.numel() < nq or t.element_size() != size or not t.is_contiguous()):
+            raise ValueError(f"ac_mx_lookup: {name} must be dense with one entry per query")
+    tab = None
+    if thresholds is not None:
+        if levels is None or len(thresholds) >= AC_MAX_K_LEVELS or len(levels) != len(thresholds) + 1:
+            raise ValueError("ac_mx_lookup: at most 15 thresholds, and one level more than thresholds")
+        tab = C.byref(k_table(thresholds, levels))
+    _check(lib.ac_mx_lookup(dtype, _ptr(queries), nq, _ptr(table), n, dim, tab, _ptr(out_idx), _ptr(out_score),
+                            _ptr(out_k), _ptr(ws), _stream(stream)))
+
+
 def packed_weight_elems(dtype, N, K):
     n = C.c_int64()
     _check(lib.dn_packed_weight_elems(dtype, N, K, C.byref(n)))
@@ -371,11 +500,11 @@ def packed_weight_elems(dtype, N, K):
 
 
 def pack_weight(dtype, w, N, K, stream=None):
-    """Row-major device weight [N][K] (dtype elements; fp32 for DN_FP8) -> a new tensor in
-    the GEMM's packed layout (for DN_FP8 a uint8 tensor: codes, then N fp32 scales)."""
+    """Row-major device weight [N][K] (dtype elements; fp32 for DN_FP8 and DN_MXFP4) -> a new tensor in
+    the GEMM's packed layout (uint8 for those two: codes, then the scales)."""
     import torch
     out = torch.empty(packed_weight_elems(dtype, N, K), device=w.device,
-                      dtype=torch.uint8 if dtype == DN_FP8 else w.dtype)
+                      dtype=torch.uint8 if dtype in (DN_FP8, DN_MXFP4) else w.dtype)
     _check(lib.dn_pack_weight(dtype, _ptr(w), N, K, _ptr(out), _stream(stream)))
     return out
 

@@ -18,6 +18,7 @@ import numpy as np
 DN_FP32 = 0
 DN_BF16 = 1
 DN_FP8 = 2
+DN_MXFP4 = 3
 
 
 @dataclass
