@@ -393,7 +393,8 @@ dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, co
  * DN_MXFP4: w is fp32 [N][K] (N % 32 == 0, K % 128 == 0), quantised as the rows of dn_mx_quantize;
  *   `out` (16-byte aligned) receives N * K / 2 bytes of E2M1 codes in the operand order of the 32x32x64
  *   matrix-core step (per 32 rows and 64-deep step the lanes' 16 bytes in 1 KB), then the scales (per 64
- *   rows and 128 deep, four bytes a lane); dn_packed_weight_elems gives the total in bytes. */
+ *   rows and 128 deep, four bytes a lane), then 8 KB that products may read and ignore;
+ *   dn_packed_weight_elems gives the total in bytes. */
 dn_status dn_packed_weight_elems(int32_t dtype, int32_t N, int32_t K, int64_t* elems);
 dn_status dn_pack_weight(int32_t dtype, const void* w, int32_t N, int32_t K, void* out, void* stream);
 

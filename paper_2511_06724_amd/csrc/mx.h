@@ -7,8 +7,8 @@
 // exponent of the largest code (2 or 8), s = 0 for a zero block; code = round(x / 2^(s - 127)), nearest
 // even, saturating at 6 / 448. A block that holds an infinity or a NaN gets s = 255 and zero codes: it
 // reads back as NaN.
-// A buffer of `rows` rows: the codes of all rows, then their scales [rows][B], then zero to 31
-// bytes that make up a multiple of 16 with 16 bytes to spare (reads of a row's scales go by 16).
+// A buffer of `rows` rows: the codes of all rows, then their scales [rows][B], then 16 to 31
+// spare bytes that make up a multiple of 16 (reads of a row's scales go by 16).
 #pragma once
 
 #include "kernels.h"

@@ -201,6 +201,35 @@ def test_linear(M, N, K, resid, f32):
         assert (np.abs(got[off:off + M * N].reshape(M, N) - want) <= tol).all()
 
 
+# the tile shapes that few tiles per CU, an even number of them and many of them choose, at depths of less than
+# their pipelines and of more than the scales that a tile holds at once; the kernel of few rows at that depth
+@pytest.mark.parametrize("M,N,K,resid,f32", [
+    (2999, 2560, 8320, "bf16", False), (2047, 1248, 8320, "f32", True), (400, 1312, 8576, "bf16", True),
+    (2999, 2560, 128, None, True), (2047, 1248, 256, "bf16", False), (900, 1312, 384, "f32", False), (40, 96, 16768, "f32", True)])
+def test_linear_tiles(M, N, K, resid, f32):
+    test_linear(M, N, K, resid, f32)
+
+
+@pytest.mark.parametrize("M,N,K,bias", [(600, 2880, 256, True), (580, 2848, 8320, False), (1999, 2560, 8320, True), (1100, 5120, 128, True),
+                                        (40, 96, 8576, True)])
+def test_linear_geglu_tiles(M, N, K, bias):
+    test_linear_geglu(M, N, K, bias)
+
+
+def test_linear_residual_in_place():
+    """y may be the residual's own memory: each value is read before it is written, by the same lanes."""
+    for M, N, K in ((5, 64, 128), (700, 1280, 256), (4096, 2560, 256)):
+        announce(f"mx4 linear in place {M}x{N}x{K}")
+        r = _rng(M, N, K, 5)
+        x, w, b, xh, wh = _operands(r, M, N, K)
+        xq, wp = dn.mx_quantize(dn.DN_MXFP4, f32_dev(x)), dn.pack_weight(dn.DN_MXFP4, f32_dev(w), N, K)
+        y = f32_dev(r.standard_normal((M, N)).astype(np.float32))
+        want = torch.empty_like(y)
+        dn.op_linear(dn.DN_MXFP4, xq, wp, f32_dev(b), want, M, N, K, resid=y, resid_f32=True, y_f32=True)
+        dn.op_linear(dn.DN_MXFP4, xq, wp, f32_dev(b), y, M, N, K, resid=y, resid_f32=True, y_f32=True)
+        assert torch.equal(y, want)
+
+
 def _check_mx(got_buf, y, delta, M, N):
     """An MX4 buffer against exact values y known to within delta: the block's scale is that of a
     largest magnitude within delta, and every value as near as the nearest code of that scale."""
