@@ -380,6 +380,15 @@ def test_lookup(fmt, n, dim, nq):
     _check_search(fmt, x, q, _search(fmt, x, q))
 
 
+# row lengths around those that change kernel or registers, odd ones whose queries begin at any address; query
+# counts around the groups of 16
+@pytest.mark.parametrize("dim", [7, 8, 9, 33, 255, 257, 512, 513, 768, 769, 1023, 1024, 1025])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_lookup_lengths_and_groups(fmt, dim):
+    for n, nq in ((1, 1), (17, 16), (1000, 17), (1030, 32), (700, 33), (1500, 64), (300, 70)):
+        test_lookup(fmt, n, dim, nq)
+
+
 @pytest.mark.parametrize("nq", [1, 2, 40])
 @pytest.mark.parametrize("dim", [96, 768, 1056])
 @pytest.mark.parametrize("fmt", FMTS)
