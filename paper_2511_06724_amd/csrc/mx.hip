@@ -1,9 +1,11 @@
 // Microscaled rows (mx.h): quantisation of rows as they are written (in order, or scattered into
 // the slots of a cache), reading back, and the packing of 4-bit weights (gfx950).
 //
-// Both directions move bytes and do little else: a thread handles eight values (16 or 32 bytes of
+// Both directions move bytes and do little else. A thread handles eight values (16 or 32 bytes of
 // the source, 4 or 8 of codes), four neighbouring lanes a block, whose largest magnitude meets in
-// two DPP steps. Every thread issues the loads of its kUnroll groups before it uses the first.
+// two DPP steps. Slots are looked up once per row and workgroup. Bound by memory where rows are many: 100000 rows of
+// 768 fp16 values into scattered slots of a table of E2M1 rows 47 us and 10 for the claims (195 MB: 38 us at
+// 5.1 TB/s; in order 36), back as fp32 87 us (348 MB, 68); with one group of eight per thread instead of two 55 and 91.
 #include <algorithm>
 
 #include "mx.h"
@@ -11,41 +13,27 @@
 namespace dn {
 namespace {
 
-constexpr int kUnroll = 4;
-constexpr int kGroups = 256 * kUnroll;  // groups of eight values per workgroup
-// Rows per call up to which a row looks for a later row of the same slot by itself; more are
-// claimed by kernels of their own.
-constexpr int kScanRows = 32;
+constexpr int kStoreUnroll = 2, kFetchUnroll = 2;
+constexpr int kStoreGroups = 256 * kStoreUnroll;  // groups of eight values per workgroup
+constexpr int kFetchGroups = 256 * kFetchUnroll;
+// Rows per call up to which every workgroup looks for later rows of its rows' slots by itself; more are
+// claimed by kernels of their own (64 states of 65536 values: 9.5 us with those).
+constexpr int kScanRows = 256;
 constexpr int kClaimOneGroup = 16384;   // rows one workgroup claims in a single launch
 
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-
-// Elements [c, c + 8) of a row, zero past `cols`.
-__device__ __forceinline__ void load8(const float* x, long long c, long long cols, bool vec, float* v) {
-  if (vec && c + 8 <= cols) {
-    const float4 a = *reinterpret_cast<const float4*>(x + c), b = *reinterpret_cast<const float4*>(x + c + 4);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  } else {
+// Elements [c, c + 8) of a row, zero past `cols`; a row may begin at any element.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Eight {
+  T v[8];
+};
+template <typename T> __device__ __forceinline__ void load8(const T* x, long long c, long long cols, float* v) {
+  if (c + 8 <= cols) {
+    const Eight<T> a = *reinterpret_cast<const Eight<T>*>(x + c);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? x[c + e] : 0.f;
-  }
-}
-template <typename H, typename H8>
-__device__ __forceinline__ void load8_16(const H* x, long long c, long long cols, bool vec, float* v) {
-  if (vec && c + 8 <= cols) {
-    const H8 a = *reinterpret_cast<const H8*>(x + c);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(a[e]);
+    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(a.v[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? static_cast<float>(x[c + e]) : 0.f;
   }
-}
-__device__ __forceinline__ void load8(const bf16* x, long long c, long long cols, bool vec, float* v) {
-  load8_16<bf16, bf16x8>(x, c, cols, vec, v);
-}
-__device__ __forceinline__ void load8(const _Float16* x, long long c, long long cols, bool vec, float* v) {
-  load8_16<_Float16, half8>(x, c, cols, vec, v);
 }
 
 __device__ __forceinline__ unsigned amax8(const float* v) {
@@ -55,23 +43,33 @@ __device__ __forceinline__ unsigned amax8(const float* v) {
   return a;
 }
 
-// Row and first value of each of a thread's groups; the row index is 64-bit, the offset in a
-// workgroup's rows 32-bit (one 64-bit division per workgroup).
-struct GroupPos {
-  long long row;
-  unsigned g;  // group of the row
-};
-struct GroupMap {
+// The value N lanes up in a row of sixteen (the last N lanes': 0).
+template <int N> __device__ __forceinline__ unsigned dpp_row_shl(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x100 + N, 0xf, 0xf, true);
+}
+
+// The groups of eight values of a workgroup that covers N of them from group `base` on, rows of per_row groups
+// one after the other: its first row, and a thread's groups, 256 apart, as row (counted from the first) and
+// group of the row. One 64-bit division per workgroup, one of 32 bits per thread.
+template <unsigned N> struct Groups {
   long long row0;
-  unsigned off, per_row;
-  __device__ GroupMap(long long base, unsigned groups_per_row) : per_row(groups_per_row) {
-    row0 = base / groups_per_row;
-    off = (unsigned)(base - row0 * groups_per_row);
+  unsigned off, per_row, rows;  // rows that it may touch
+  unsigned row, g, dq, dr;
+  __device__ Groups(long long base, unsigned groups_per_row, long long rows_all) : per_row(groups_per_row) {
+    row0 = base / per_row;
+    off = (unsigned)(base - row0 * per_row);
+    rows = (unsigned)min((long long)((off + N - 1) / per_row + 1), rows_all - row0);
+    const unsigned t = off + threadIdx.x;
+    row = t / per_row;
+    g = t - row * per_row;
+    dq = 256 / per_row;
+    dr = 256 - dq * per_row;
   }
-  __device__ GroupPos at(unsigned local) const {
-    const unsigned t = off + local;
-    const unsigned q = per_row >= kGroups ? (t >= per_row ? 1u : 0u) : t / per_row;
-    return GroupPos{row0 + q, t - q * per_row};
+  __device__ void next() {
+    g += dr;
+    const bool wrap = g >= per_row;
+    row += dq + wrap;
+    g -= wrap ? per_row : 0;
   }
 };
 
@@ -79,7 +77,6 @@ struct StoreParams {
   const void* x;
   long long ldx, rows, cols;
   unsigned blocks;          // of a row
-  int vec;                  // rows can be read 16 bytes at a time
   const long long* slots;   // nullptr: row j goes to slot j
   long long n_slots;
   const int* owner;         // nullptr: rows look for later rows of their slot themselves
@@ -87,45 +84,66 @@ struct StoreParams {
   unsigned char* scales;
 };
 
-// Destination of row j, -1 for none (a slot outside the table, or a later row of the same slot).
-__device__ __forceinline__ long long store_slot(const StoreParams& p, long long j) {
-  if (!p.slots) return j;
-  const long long s = p.slots[j];
-  if (s < 0 || s >= p.n_slots) return -1;
-  if (p.owner) return p.owner[s] == (int)j ? s : -1;
-  for (long long k = j + 1; k < p.rows; ++k)
-    if (p.slots[k] == s) return -1;
-  return s;
+// First block of the destination of rows row0 .. row0 + n - 1, -1 for none (a slot outside the table, or a later
+// row of the same slot), into LDS.
+__device__ __forceinline__ void store_blocks(const StoreParams& p, long long row0, unsigned n, long long* first, long long* all) {
+  const int t = threadIdx.x;
+  if (p.owner) {
+    for (unsigned i = t; i < n; i += 256) {
+      const long long s = p.slots[row0 + i];
+      first[i] = s >= 0 && s < p.n_slots && p.owner[s] == (int)(row0 + i) ? s * p.blocks : -1;
+    }
+  } else {
+    if (t < p.rows) all[t] = p.slots[t];
+    __syncthreads();
+    for (unsigned i = t; i < n; i += 256) {
+      const int j = (int)row0 + (int)i;
+      const long long s = all[j];
+      bool on = s >= 0 && s < p.n_slots;
+#pragma unroll 8
+      for (int k = j + 1; k < (int)p.rows; ++k) on &= all[k] != s;
+      first[i] = on ? s * p.blocks : -1;
+    }
+  }
+  __syncthreads();
 }
 
 template <int FMT, typename T> __global__ __launch_bounds__(256) void mx_store_kernel(StoreParams p) {
-  const unsigned G = p.blocks * 4;
-  const long long base = (long long)blockIdx.x * kGroups, total = p.rows * G;
-  const GroupMap map(base, G);
-  float v[kUnroll][8];
-  GroupPos pos[kUnroll];
-  long long slot[kUnroll];
+  __shared__ long long first[kStoreGroups / 4 + 1], all[kScanRows];
+  const long long base = (long long)blockIdx.x * kStoreGroups, total = p.rows * (p.blocks * 4ll);
+  Groups<kStoreGroups> at(base, p.blocks * 4, p.rows);
+  const T* const x = static_cast<const T*>(p.x) + at.row0 * p.ldx;
+  float v[kStoreUnroll][8];
+  unsigned row[kStoreUnroll], g[kStoreUnroll];
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    const unsigned local = u * 256 + threadIdx.x;
-    slot[u] = -1;
-    if (base + local >= total) continue;
-    pos[u] = map.at(local);
-    load8(static_cast<const T*>(p.x) + pos[u].row * p.ldx, 8ll * pos[u].g, p.cols, p.vec, v[u]);
-    slot[u] = store_slot(p, pos[u].row);
+  for (int u = 0; u < kStoreUnroll; ++u) {
+    row[u] = at.row, g[u] = at.g;
+    at.next();
+    if (base + u * 256 + threadIdx.x < total) load8(x + row[u] * p.ldx, 8ll * g[u], p.cols, v[u]);
   }
+  if (p.slots) store_blocks(p, at.row0, at.rows, first, all);
+  // every load arrives before the first store is out: a wait for a load after it would wait for the store too
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    if (slot[u] < 0) continue;  // the four lanes of a block together
+  for (int u = 0; u < kStoreUnroll; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(v[u][e]));
+#pragma unroll
+  for (int u = 0; u < kStoreUnroll; ++u) {
+    if (base + u * 256 + threadIdx.x >= total) break;  // the four lanes of a block together, here and below
+    const long long b0 = p.slots ? first[row[u]] : (at.row0 + row[u]) * p.blocks;
+    if (b0 < 0) continue;
     const unsigned s = mx_scale<FMT>(quad_umax(amax8(v[u])));
-    const long long block = slot[u] * p.blocks + pos[u].g / 4;
-    if constexpr (FMT == kMx4) {
-      *reinterpret_cast<unsigned*>(p.codes + block * 16 + (pos[u].g & 3) * 4) = mx4_codes8(v[u], s);
-    } else {
-      *reinterpret_cast<uint2*>(p.codes + block * 32 + (pos[u].g & 3) * 8) =
-          make_uint2(mx8_codes4(v[u], s), mx8_codes4(v[u] + 4, s));
+    if constexpr (FMT == kMx4)
+      *reinterpret_cast<unsigned*>(p.codes + b0 * 16 + g[u] * 4ull) = mx4_codes8(v[u], s);
+    else
+      *reinterpret_cast<uint2*>(p.codes + b0 * 32 + g[u] * 8ull) = make_uint2(mx8_codes4(v[u], s), mx8_codes4(v[u] + 4, s));
+    if (p.blocks % 4 == 0) {
+      // sixteen lanes hold four blocks of a row, whose scales are a word
+      const unsigned w = s | dpp_row_shl<4>(s) << 8 | dpp_row_shl<8>(s) << 16 | dpp_row_shl<12>(s) << 24;
+      if ((g[u] & 15) == 0) *reinterpret_cast<unsigned*>(p.scales + b0 + g[u] / 4) = w;
+    } else if ((g[u] & 3) == 0) {
+      p.scales[b0 + g[u] / 4] = (unsigned char)s;
     }
-    if ((pos[u].g & 3) == 0) p.scales[block] = (unsigned char)s;
   }
 }
 
@@ -160,35 +178,42 @@ struct FetchParams {
   const long long* idx;  // nullptr: row j is slot j
   float* y;
   long long ldy;
-  int vec;
 };
 
+// Four values at any address, as one store (of a structure, the compiler splits one off for the short path).
+typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+
 template <int FMT> __global__ __launch_bounds__(256) void mx_fetch_kernel(FetchParams p) {
-  const unsigned G = p.blocks * 4;
-  const long long base = (long long)blockIdx.x * kGroups, total = p.rows * G;
-  const GroupMap map(base, G);
-  GroupPos pos[kUnroll];
-  bool on[kUnroll];
-  uint2 code[kUnroll];
-  unsigned s[kUnroll];
-#pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    const unsigned local = u * 256 + threadIdx.x;
-    on[u] = base + local < total;
-    if (!on[u]) continue;
-    pos[u] = map.at(local);
-    const long long slot = p.idx ? p.idx[pos[u].row] : pos[u].row;
-    on[u] = slot >= 0 && slot < p.n_slots;
-    if (!on[u]) continue;
-    const long long block = slot * p.blocks + pos[u].g / 4;
-    if constexpr (FMT == kMx4)
-      code[u].x = *reinterpret_cast<const unsigned*>(p.codes + block * 16 + (pos[u].g & 3) * 4);
-    else
-      code[u] = *reinterpret_cast<const uint2*>(p.codes + block * 32 + (pos[u].g & 3) * 8);
-    s[u] = p.scales[block];
+  __shared__ long long first[kFetchGroups / 4 + 1];
+  const long long base = (long long)blockIdx.x * kFetchGroups, left = p.rows * (p.blocks * 4ll) - base;
+  Groups<kFetchGroups> at(base, p.blocks * 4, p.rows);
+  if (p.idx) {
+    for (unsigned i = threadIdx.x; i < at.rows; i += 256) {
+      const long long s = p.idx[at.row0 + i];
+      first[i] = s >= 0 && s < p.n_slots ? s * p.blocks : -1;
+    }
+    __syncthreads();
   }
+  unsigned row[kFetchUnroll], g[kFetchUnroll], s[kFetchUnroll];
+  bool on[kFetchUnroll];
+  uint2 code[kFetchUnroll];
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
+  for (int u = 0; u < kFetchUnroll; ++u) {
+    row[u] = min(at.row, at.rows - 1), g[u] = at.g;
+    at.next();
+    const long long b = p.idx ? first[row[u]] : (at.row0 + row[u]) * p.blocks, b0 = max(b, 0ll);  // none: read block 0
+    on[u] = u * 256 + threadIdx.x < left && b >= 0;
+    if constexpr (FMT == kMx4)
+      code[u] = make_uint2(*reinterpret_cast<const unsigned*>(p.codes + b0 * 16 + g[u] * 4ull), 0u);
+    else
+      code[u] = *reinterpret_cast<const uint2*>(p.codes + b0 * 32 + g[u] * 8ull);
+    s[u] = p.scales[b0 + g[u] / 4];
+  }
+  // every load arrives before the first store is out: a wait for a load after it would wait for the store too
+#pragma unroll
+  for (int u = 0; u < kFetchUnroll; ++u) asm volatile("" : "+v"(code[u].x), "+v"(code[u].y), "+v"(s[u]));
+#pragma unroll
+  for (int u = 0; u < kFetchUnroll; ++u) {
     if (!on[u]) continue;
     float v[8];
     if constexpr (FMT == kMx4) {
@@ -197,14 +222,14 @@ template <int FMT> __global__ __launch_bounds__(256) void mx_fetch_kernel(FetchP
       mx8_values4(code[u].x, s[u], v);
       mx8_values4(code[u].y, s[u], v + 4);
     }
-    const long long c = 8ll * pos[u].g;
-    float* y = p.y + pos[u].row * p.ldy + c;
-    if (p.vec && c + 8 <= p.cols) {
-      *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(y + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    const unsigned c = 8 * g[u], cols = (unsigned)p.cols;
+    float* const y = p.y + (at.row0 + row[u]) * p.ldy + c;
+    if (c + 8 <= cols) {
+      reinterpret_cast<Four*>(y)[0] = Four{v[0], v[1], v[2], v[3]};
+      reinterpret_cast<Four*>(y)[1] = Four{v[4], v[5], v[6], v[7]};
     } else {
-      for (int e = 0; e < 8; ++e)
-        if (c + e < p.cols) y[e] = v[e];
+      for (unsigned e = 0; e < 8; ++e)
+        if (c + e < cols) y[e] = v[e];
     }
   }
 }
@@ -229,8 +254,8 @@ __global__ __launch_bounds__(256) void pack_mx4_kernel(PackParams p, unsigned ch
   if ((c & 31) == 0) scales[(quad * 64 + lane) * 4 + ((r >> 5) & 1) * 2 + ((c >> 6) & 1)] = (unsigned char)s;
 }
 
-unsigned grid_for(long long groups) {
-  const long long n = (groups + kGroups - 1) / kGroups;
+unsigned grid_for(long long groups, int per_workgroup) {
+  const long long n = (groups + per_workgroup - 1) / per_workgroup;
   DN_CHECK(n <= 0x7fffffffll, "mx: too many values for one call");
   return static_cast<unsigned>(n);
 }
@@ -257,13 +282,12 @@ void mx_store(int fmt, const T* x, long long ldx, long long rows, long long cols
   p.rows = rows;
   p.cols = cols;
   p.blocks = static_cast<unsigned>(mx_blocks(cols));
-  p.vec = (reinterpret_cast<uintptr_t>(x) | (uintptr_t)ldx * sizeof(T)) % 16 == 0;
   p.slots = slots;
   p.n_slots = n_slots;
   p.owner = rows > kScanRows ? owner : nullptr;
   p.codes = static_cast<unsigned char*>(table);
   p.scales = p.codes + mx_scale_offset(fmt, n_slots, cols);
-  const unsigned grid = grid_for(rows * p.blocks * 4);
+  const unsigned grid = grid_for(rows * p.blocks * 4, kStoreGroups);
   if (slots && rows > kScanRows) {
     if (rows <= kClaimOneGroup) {
       hipLaunchKernelGGL(mx_claim_kernel<0>, dim3(1), dim3(1024), 0, s, slots, rows, n_slots, owner);
@@ -292,8 +316,7 @@ void mx_fetch(int fmt, const void* table, long long n_slots, long long cols, con
   p.idx = idx;
   p.y = y;
   p.ldy = ldy;
-  p.vec = (reinterpret_cast<uintptr_t>(y) | (uintptr_t)ldy * 4) % 16 == 0;
-  const unsigned grid = grid_for(rows * p.blocks * 4);
+  const unsigned grid = grid_for(rows * p.blocks * 4, kFetchGroups);
   if (fmt == kMx4)
     hipLaunchKernelGGL(mx_fetch_kernel<kMx4>, dim3(grid), dim3(256), 0, s, p);
   else

@@ -129,6 +129,35 @@ def test_store_and_fetch(fmt, n, n_slots, dim):
     assert (out[:, dim:] == -3.0).all()
 
 
+# a workgroup's share of one row, of two and of many; whole words of scales and single ones; the most rows whose
+# slots workgroups compare by themselves, and one more
+@pytest.mark.parametrize("n,n_slots,dim", [(5, 9, 65536), (3, 4, 4097), (64, 70, 5120), (200, 90, 128), (255, 300, 32), (256, 120, 1),
+                                           (256, 40, 2560), (257, 130, 64), (600, 650, 777)])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_store_and_fetch_shapes(fmt, n, n_slots, dim):
+    test_store_and_fetch(fmt, n, n_slots, dim)
+
+
+def test_fetch_and_store_rows_at_any_element():
+    """Sources and targets whose rows begin at every element of a 16-byte word, of every type."""
+    announce("mx rows at odd addresses")
+    r = _rng(77)
+    for dt in (torch.float32, torch.bfloat16, torch.float16):
+        for cols in (8, 61, 256):
+            for off in range(8):
+                x = torch.from_numpy(r.standard_normal((9, cols + off)).astype(np.float32)).to(dt)
+                dev = torch.zeros(off + x.numel(), device=DEV, dtype=dt)[off:].view(9, cols + off).copy_(x)[:, :cols]
+                want = mx.rounded(x[:, :cols].double().numpy(), mx.MXFP8)
+                table = _u8(dn.mx_bytes(dn.DN_MXFP8, 9, cols), 0)
+                dn.ac_mx_store(dn.DN_MXFP8, dev, torch.arange(9, device=DEV), table, 9)
+                out = torch.full((off + 9 * (cols + off),), 2.5, device=DEV)
+                view = out[off:].view(9, cols + off)[:, :cols]
+                dn.ac_mx_fetch(dn.DN_MXFP8, table, 9, torch.arange(8, -1, -1, device=DEV), view)
+                assert np.array_equal(host(view), want[::-1])
+                view.fill_(2.5)
+                assert (host(out) == 2.5).all()
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 def test_tables_past_32_bits(fmt):
     """Slots whose codes begin past 2^32 bytes: stored, read back and (as embeddings) found."""

@@ -61,7 +61,7 @@ def test_dequantize_refused(change):
     assert dn.lib.dn_mx_dequantize(a["dtype"], a["q"], a["rows"], a["cols"], a["y"], a["ldy"], None) == dn.DN_EINVAL
 
 
-STORE = dict(dtype=dn.DN_MXFP4, src=dn.DN_FP32, x=P, ldx=64, n=40, slots=P, table=P, n_slots=100, dim=64, ws=P)
+STORE = dict(dtype=dn.DN_MXFP4, src=dn.DN_FP32, x=P, ldx=64, n=400, slots=P, table=P, n_slots=100, dim=64, ws=P)
 
 
 @pytest.mark.parametrize("change", [dict(dtype=1), dict(src=4), dict(x=None), dict(slots=None), dict(table=None), dict(ws=None),
