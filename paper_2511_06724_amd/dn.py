@@ -7,6 +7,7 @@ module raises if the library has not been built: there is no fallback.
 """
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -150,10 +151,21 @@ def _ptr(t):
     return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=None)
+def _raw_stream():
+    """Function that gives the current stream's handle. torch.cuda.current_stream() builds an object first,
+    2.8 us of a call whose launch takes 3."""
+    import torch
+    device, raw = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if device is None or raw is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    torch.cuda.init()
+    return lambda: raw(device())
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _raw_stream()()
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -375,6 +387,8 @@ def ac_fetch_latent(cache_latents, idx, latent, stream=None):
 
 # ----------------------------------------------------------------------------- microscaled rows
 
+# Sizes are functions of their arguments; calls check buffers against them each time.
+@functools.lru_cache(maxsize=1024)
 def mx_bytes(dtype, rows, cols):
     """Bytes of an MX buffer (DN_MXFP4 or DN_MXFP8) of `rows` rows of `cols` values."""
     n = C.c_int64()
@@ -382,20 +396,28 @@ def mx_bytes(dtype, rows, cols):
     return n.value
 
 
+@functools.lru_cache(maxsize=None)
+def _row_types():
+    import torch
+    return {torch.float32: DN_FP32, torch.bfloat16: DN_BF16, torch.float16: DN_FP16}
+
+
 def _rows(x, name):
     """(dtype, row stride, rows, columns) of a row source: a 2-D tensor whose rows are dense."""
-    import torch
-    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+    if x.dim() != 2:
         raise ValueError(f"{name}: a 2-D tensor with dense rows is needed")
-    dt = {torch.float32: DN_FP32, torch.bfloat16: DN_BF16, torch.float16: DN_FP16}.get(x.dtype)
+    (rows, cols), (ld, step) = x.shape, x.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{name}: a 2-D tensor with dense rows is needed")
+    dt = _row_types().get(x.dtype)
     if dt is None:
         raise ValueError(f"{name}: rows must be float32, bfloat16 or float16")
-    return dt, max(x.stride(0), x.shape[1]) if x.shape[0] == 1 else x.stride(0), x.shape[0], x.shape[1]
+    return dt, max(ld, cols) if rows == 1 else ld, rows, cols
 
 
 def _buffer(t, need, name):
     """Checks a caller's byte buffer (uint8, dense) against the bytes a call accesses."""
-    if t.numel() * t.element_size() < need or not t.is_contiguous():
+    if t.nbytes < need or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous buffer of at least {need} bytes is needed")
 
 
@@ -431,6 +453,7 @@ def mx_dequantize(dtype, q, rows, cols, y=None, stream=None):
     return y
 
 
+@functools.lru_cache(maxsize=1024)
 def ac_mx_store_bytes(n_rows, n_slots):
     """Workspace bytes of ac_mx_store (0: none is needed)."""
     n = C.c_int64()
@@ -464,6 +487,7 @@ def ac_mx_fetch(dtype, table, n_slots, idx, out, stream=None):
     _check(lib.ac_mx_fetch(dtype, _ptr(table), n_slots, dim, _ptr(idx), n, _ptr(out), ldo, _stream(stream)))
 
 
+@functools.lru_cache(maxsize=1024)
 def ac_mx_lookup_bytes(nq, n, dim):
     """Workspace bytes of ac_mx_lookup."""
     b = C.c_int64()

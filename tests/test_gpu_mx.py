@@ -480,6 +480,19 @@ def test_lookup_levels_are_those_of_the_reported_cosine():
 
 # ----------------------------------------------------------------------------- together
 
+def test_calls_without_a_stream_take_the_current_one():
+    announce("current stream")
+    side = torch.cuda.Stream()
+    for _ in range(2):
+        assert dn._stream(None) == torch.cuda.current_stream().cuda_stream
+        with torch.cuda.stream(side):
+            assert dn._stream(None) == side.cuda_stream == dn._stream(side)
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                assert dn._stream(None) == torch.cuda.current_stream().cuda_stream != side.cuda_stream
+                torch.zeros(1, device=DEV)
+
+
 def test_streams_and_graphs():
     """Store, search, fetch and the feed-forward on a side stream and captured into two graphs with
     workspaces of their own, replayed in turn: every result equals the eager one bit for bit."""
