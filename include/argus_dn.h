@@ -416,7 +416,8 @@ dn_status dn_pack_weight(int32_t dtype, const void* w, int32_t N, int32_t K, voi
  * DN_MXFP4: x an MX buffer (dn_mx_quantize) of M rows of K values, w packed for DN_MXFP4 (K % 128 == 0,
  *   N % 32 == 0; GEGLU rows interleaved as above before packing); y fp32 when y_f32 != 0, else for
  *   geglu != 0 an MX buffer of M rows of N values (the input of the next layer), else bf16; resid fp32 or
- *   bf16 per resid_f32. A NaN block of x or w makes the outputs it enters NaN. No workspace. x, w and an MX output
+ *   bf16 per resid_f32. A NaN block of x or w makes the outputs it enters NaN. No workspace. N (GEGLU: 2N) and K
+ *   at most 2^22; y may be resid if both have one type. x, w and an MX output
  *   16-byte aligned; other buffers aligned to their elements. */
 dn_status dn_op_linear(int32_t dtype, const void* x, const void* w, const float* bias, const void* resid,
                        int32_t resid_f32, void* y, int32_t y_f32, int64_t M, int32_t N, int32_t K, int32_t geglu,

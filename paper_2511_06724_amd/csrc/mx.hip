@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256) void pack_mx4_kernel(PackParams p, unsigned ch
 
 unsigned grid_for(long long groups, int per_workgroup) {
   const long long n = (groups + per_workgroup - 1) / per_workgroup;
-  DN_CHECK(n <= 0x7fffffffll, "mx: too many values for one call");
+  DN_CHECK(n <= 0xffffffll, "mx: too many values for one call");  // a launch has less than 2^32 threads
   return static_cast<unsigned>(n);
 }
 

@@ -7,8 +7,8 @@
 //
 // Rows of 8 .. 1024 values (mx_scan_mfma_kernel): codes converted to fp16 (exact) against up to 64 queries
 // held in registers, on the matrix cores; the table is read once per pass, 17/32 (33/32) bytes a value.
-// Bound by that for few queries: 100000 x 768 E2M1 rows (41 MB) 13.6 us with the reduction for one query (one
-// pass at 5.1 TB/s: 8.0), 14.6 for 16; a million rows 73.7 (79.7). For 64 queries 21.7: a third of it the
+// Bound by that for few queries: 100000 x 768 E2M1 rows (41 MB) 13.1 us with the reduction for one query (one
+// pass at 5.1 TB/s: 8.0), 13.9 for 16; a million rows 73.4 (79.7). For 64 queries 21.8: a third of it the
 // queries' way into the registers of every CU (98 KB each), the rest products and conversions (16 cycles per
 // product, 8 per conversion of two values).
 // Other rows (mx_scan_kernel): one or two queries per pass, packed dot products in fp32.
@@ -408,16 +408,27 @@ __global__ __launch_bounds__(256) void mx_reduce_kernel(const Cand* part, int nb
   const int j = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
   float bs = -INFINITY, qq = 0.f;
   long long bi = n;
-  for (int k = t; k < nb; k += 256) {
-    const Cand c = part[(long long)k * pitch + j];
+  // few iterations of many loads: in a chain of dependent ones the latency of each would be most of the kernel
+  const _Float16* const qj = q + (long long)j * dim;
+  for (int k = t; k < nb; k += 512) {
+    const Cand c = part[(long long)k * pitch + j], d = part[(long long)min(k + 256, nb - 1) * pitch + j];
     if (better(c.s, c.i, bs, bi)) {
       bs = c.s;
       bi = c.i;
     }
+    if (better(d.s, d.i, bs, bi)) {
+      bs = d.s;
+      bi = d.i;
+    }
   }
-  for (int e = t; e < dim; e += 256) {
-    const float x = static_cast<float>(q[(long long)j * dim + e]);
-    qq += x * x;
+  if (dim >= 8) {
+    for (int e = 8 * t; e < dim; e += 2048) {
+      const f16x8 x = query_value(query_load(qj, e, dim));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qq = fmaf(static_cast<float>(x[i]), static_cast<float>(x[i]), qq);
+    }
+  } else if (t < dim) {
+    qq = static_cast<float>(qj[t]) * static_cast<float>(qj[t]);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {

@@ -433,6 +433,24 @@ def test_lookup_scales_of_any_size(fmt, dim, nq):
     _check_search(fmt, x, q, _search(fmt, x, q))
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -22, 2.0 ** -14, 2.0 ** 12])
+@pytest.mark.parametrize("dim", [5, 64, 768, 1100])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_lookup_queries_of_any_size(fmt, dim, scale):
+    """Queries of fp16 values below its normal range and near its largest: cosines of what they hold."""
+    announce(f"mx lookup, queries of size {scale} fmt={fmt} dim={dim}")
+    for nq in (1, 20):
+        x, q = _planted(_rng(dim, nq, 6), 300, dim, nq)
+        q = (q.astype(np.float64) * scale).astype(np.float16)
+        q[0, 0] = np.float16(scale)
+        idx, score, _ = _search(fmt, x, q)
+        # a component of a unit vector below 2^-3 is below half of fp16's least, 2^-24, when scaled by 2^-22, hence
+        # some queries hold zeros only, and a zero query finds nothing
+        on = (q != 0).any(1)
+        assert on[0] and (idx[~on] == -1).all() and (score[~on] == 0).all()
+        _check_search(fmt, x, q[on], (idx[on], score[on], None))
+
+
 @pytest.mark.parametrize("n,nq", [(200, 1), (200, 3), (200, 64), (5000, 2), (5000, 33)])
 @pytest.mark.parametrize("dim", [64, 768, 1100])
 @pytest.mark.parametrize("fmt", FMTS)

@@ -142,3 +142,12 @@ def test_binding_checks_buffers_and_strides():
               lambda: dn.ac_mx_fetch(dn.DN_MXFP4, torch.zeros(99, dtype=torch.uint8), 9, torch.zeros(4, dtype=torch.int64), x, stream=0)):
         with pytest.raises(ValueError):
             f()
+
+
+def test_too_large_for_one_launch_refused():
+    """More work than a launch has threads, and offsets in a tile's rows past 32 bits."""
+    rows, cols = 2 ** 31 - 1, 320
+    assert dn.lib.dn_mx_quantize(dn.DN_MXFP4, dn.DN_FP32, P, cols, rows, cols, P, None) == dn.DN_EINVAL
+    assert dn.lib.dn_mx_dequantize(dn.DN_MXFP8, P, rows, cols, P, cols, None) == dn.DN_EINVAL
+    for n, k in ((2 ** 22 + 32, 128), (32, 2 ** 22 + 128)):
+        assert dn.lib.dn_op_linear(dn.DN_MXFP4, P, P, None, None, 0, P, 1, 1, n, k, 0, None) == dn.DN_EINVAL
