@@ -1,6 +1,7 @@
 // C ABI of the denoise-loop library: argument checks, error mapping and the
 // single-kernel entry points. Every entry point catches all C++ exceptions.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -252,9 +253,12 @@ void grow(float** buf, size_t* have, size_t need) {
 
 // Compute units of the current device (no allocation: callers may be capturing).
 int current_cus() {
+  static std::atomic<int> known[64];  // by device; asking takes most of a microsecond
   int dev = 0, cus = 0;
   DN_HIP(hipGetDevice(&dev));
+  if (dev < 64 && (cus = known[dev].load(std::memory_order_relaxed))) return cus;
   DN_HIP(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
+  if (dev < 64) known[dev].store(cus, std::memory_order_relaxed);
   return cus;
 }
 

@@ -10,6 +10,7 @@
 //    position c ^ ((r / 4) % 4), so that sixteen consecutive rows' reads of a chunk touch all banks;
 //  - C^T = B A^T, a lane then holds four consecutive columns of a row per register group;
 //  - tiles go to XCDs in contiguous ranges, row tiles fastest, so that a band of B stays in one L2.
+#include <algorithm>
 #include <type_traits>
 
 #include "lane_swap.h"
@@ -514,13 +515,28 @@ __device__ __forceinline__ void mx4_tile(const GemmMx4Params& p, const int m0, c
   }
 }
 
+// Workgroup wg of `units` tiles, in contiguous ranges per XCD.
+__device__ __forceinline__ int xcd_unit(int wg, int units) {
+  const int xcd = wg % kXcds, idx = wg / kXcds;
+  return xcd * (units / kXcds) + min(xcd, units % kXcds) + idx;
+}
+
 template <int FM, int FN, int S, int NW, bool GE>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_mx4_kernel(GemmMx4Params p, int mt, int nt) {
-  const int wg = blockIdx.x, units = mt * nt;
-  const int xcd = wg % kXcds, idx = wg / kXcds;
-  const int base = units / kXcds, rem = units % kXcds;
-  const int u = xcd * base + min(xcd, rem) + idx;
+  const int u = xcd_unit(blockIdx.x, mt * nt);
   mx4_tile<FM, FN, S, NW, GE>(p, (u % mt) * 32 * FM, (u / mt) * 32 * FN * NW);
+}
+
+// GEGLU: the first nt column bands in mt tiles of 128 rows, then bands in mt2 tiles of 64 rows.
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_mx4_geglu_kernel(GemmMx4Params p, int mt, int nt, int mt2) {
+  const int big = mt * nt, wg = blockIdx.x;
+  if (wg < big) {
+    const int u = xcd_unit(wg, big);
+    mx4_tile<4, 2, 3, 4, true>(p, (u % mt) * 128, (u / mt) * 256);
+  } else {
+    const int u = xcd_unit(wg - big, gridDim.x - big);
+    mx4_tile<2, 2, 4, 4, true>(p, (u % mt2) * 64, (nt + u / mt2) * 256);
+  }
 }
 
 // ---------------------------------------------------------------- few rows
@@ -617,6 +633,15 @@ template <int FM, int FN, int S, int NW, bool GE> void launch_tile(const GemmMx4
   hipLaunchKernelGGL((gemm_mx4_kernel<FM, FN, S, NW, GE>), dim3(mt * nt), dim3(64 * NW), lds, s, p, mt, nt);
 }
 
+// GEGLU with the last `small` column bands in tiles of 64 rows.
+void launch_geglu(const GemmMx4Params& p, int small, hipStream_t s) {
+  const size_t lds = std::max(tile_lds<4, 3>(p.K), tile_lds<2, 4>(p.K));
+  const int mt = ceil_div(p.M, 128), mt2 = ceil_div(p.M, 64), nt = ceil_div(p.N, 256) - small;
+  const long long grid = (long long)mt * nt + (long long)mt2 * small;
+  DN_CHECK(grid <= 0x7fffffffll, "gemm_mx4: too many tiles");
+  hipLaunchKernelGGL(gemm_mx4_geglu_kernel, dim3((unsigned)grid), dim3(256), lds, s, p, mt, nt, mt2);
+}
+
 template <bool GE> void launch_rows(const GemmMx4Params& p, hipStream_t s) {
   constexpr int NW = 8;
   const int nt = p.N / (GE ? 64 : 32), mt = ceil_div(p.M, 32);
@@ -666,11 +691,17 @@ void gemm_mx4(const GemmMx4Params& p, int cus, hipStream_t s) {
     p.geglu ? launch_rows<true>(p, s) : launch_rows<false>(p, s);
   } else if (p.geglu) {
     // 64-row tiles while all of them run at once, each on a CU of its own (300 x 2560, K = 640: 5.6 us, 128 rows
-    // 7.2); with more, 128 rows are faster (8192 x 2560, K = 640: 33.7 and 29.0)
-    if ((long long)ceil_div(p.M, 64) * ceil_div(p.N, 256) <= cus)
-      launch_tile<2, 2, 4, 4, true>(p, s);
-    else
-      launch_tile<4, 2, 3, 4, true>(p, s);
+    // 7.2); with more, 128 rows are faster (8192 x 2560, K = 640: 33.7 and 29.0). After whole rounds of two tiles
+    // per CU, a last one of half the CUs or fewer runs as 64-row tiles on twice as many (2048 x 5120, K = 1280:
+    // 24.8 and 22.4 us; with all CUs in it there is nothing to gain: 8192 x 2560, K = 640: 28.8 and 29.5)
+    const int mt = ceil_div(p.M, 128), nt = ceil_div(p.N, 256);
+    const long long tiles = (long long)mt * nt, tail = tiles % (2 * cus);
+    int small = 0;
+    if ((long long)ceil_div(p.M, 64) * nt <= cus)
+      small = nt;
+    else if (2 * tail <= cus)
+      small = (int)((tail + mt - 1) / mt);
+    launch_geglu(p, small, s);
   } else {
     // 128 x 256 does most work per byte from LDS and L2 (4096^3 39.8 us, 64 x 128 58, 64 x 160 68); the smaller
     // ones win where they even out the tiles per CU (2048 x 1280, K = 5120: 24.5, 19.8, 15.0; 700 x 1280,

@@ -402,6 +402,12 @@ def _row_types():
     return {torch.float32: DN_FP32, torch.bfloat16: DN_BF16, torch.float16: DN_FP16}
 
 
+@functools.lru_cache(maxsize=None)
+def _int64():
+    import torch
+    return torch.int64
+
+
 def _rows(x, name):
     """(dtype, row stride, rows, columns) of a row source: a 2-D tensor whose rows are dense."""
     if x.dim() != 2:
@@ -422,8 +428,7 @@ def _buffer(t, need, name):
 
 
 def _index(t, name):
-    import torch
-    if t.dtype != torch.int64 or t.dim() != 1 or not t.is_contiguous():
+    if t.dtype is not _int64() or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{name}: a dense 1-D int64 tensor is needed")
 
 

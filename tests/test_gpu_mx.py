@@ -239,7 +239,7 @@ def test_linear_tiles(M, N, K, resid, f32):
     test_linear(M, N, K, resid, f32)
 
 
-@pytest.mark.parametrize("M,N,K,bias", [(600, 2880, 256, True), (580, 2848, 8320, False), (1999, 2560, 8320, True), (1100, 5120, 128, True),
+@pytest.mark.parametrize("M,N,K,bias", [(2048, 5120, 128, True), (1990, 5056, 384, True), (8100, 1280, 256, False), (600, 2880, 256, True), (580, 2848, 8320, False), (1999, 2560, 8320, True), (1100, 5120, 128, True),
                                         (40, 96, 8576, True)])
 def test_linear_geglu_tiles(M, N, K, bias):
     test_linear_geglu(M, N, K, bias)
