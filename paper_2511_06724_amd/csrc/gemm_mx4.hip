@@ -4,12 +4,17 @@
 // supplies row (l % 32) and block (l / 32) of a 64-deep step, which is exactly a block of an MX row,
 // so operands go from memory to the matrix core without a conversion, and the sums are fp32.
 //  - B, the packed weights (pack_mx4): per 32 columns and step the lanes' 16 bytes in 1 KB of
-//    contiguous memory, loaded straight into registers D stages ahead;
-//  - A, MX rows: stages of 128 values (64 bytes of codes and 4 of scales a row) go global -> LDS
-//    without passing registers, shared by the four waves; 16-byte chunk c of row r lies at
-//    position c ^ ((r / 4) % 4), so that sixteen consecutive rows' reads of a chunk touch all banks;
+//    contiguous memory, loaded straight into registers three or four stages ahead;
+//  - A, MX rows: stages of 128 values (64 bytes of codes a row) go global -> LDS without passing
+//    registers, shared by the waves; 16-byte chunk c of row r lies at position c ^ ((r / 4) % 4), so
+//    that sixteen consecutive rows' reads of a chunk touch all banks. The scales are copied once;
 //  - C^T = B A^T, a lane then holds four consecutive columns of a row per register group;
 //  - tiles go to XCDs in contiguous ranges, row tiles fastest, so that a band of B stays in one L2.
+// A step takes the matrix core 32 cycles, at the rate of 4.9e15 operations per second that is four times a
+// large bf16 product's. Measured: 4096^3 39 us (3.5e15); 2048 x 1280, K = 5120, fp32 residual and output 15.7 us;
+// GEGLU 2048 x 5120, K = 1280 22.4 us; 32768 x 5120, K = 640 116.5 us (336 MB of output, 2.9 TB/s). The main
+// loop keeps the matrix cores 75 to 88 % busy; a tile's start (3.5 to 8 thousand cycles) and its stores and GELUs
+// (4 to 8) are what bounds the rest.
 #include <algorithm>
 #include <type_traits>
 
