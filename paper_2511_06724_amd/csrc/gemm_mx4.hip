@@ -647,6 +647,8 @@ template <int FM, int FN, int S, int NW, bool GE> void launch_tile(const GemmMx4
 
 // GEGLU with the last `small` column bands in tiles of 64 rows.
 void launch_geglu(const GemmMx4Params& p, int small, hipStream_t s) {
+  static_assert(3 * stage_bytes<4>() + scale_lds(128, kScaleK) <= 64 * 1024 && 4 * stage_bytes<2>() + scale_lds(64, kScaleK) <= 64 * 1024,
+                "no attribute needed, two workgroups per CU");
   const size_t lds = std::max(tile_lds<4, 3>(p.K), tile_lds<2, 4>(p.K));
   const int mt = ceil_div(p.M, 128), mt2 = ceil_div(p.M, 64), nt = ceil_div(p.N, 256) - small;
   const long long grid = (long long)mt * nt + (long long)mt2 * small;
