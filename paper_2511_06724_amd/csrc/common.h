@@ -156,10 +156,11 @@ constexpr int wait_vm_lgkm0(int vm) { return (vm & 0xF) | (((vm >> 4) & 3) << 14
 // register prefetch with every LDS stage. The LDS data this writes is guarded by the
 // kernel's own waits and barriers (hand-overs, and a full drain before the LDS is reused
 // for something else); it writes no VGPRs. M0 holds the LDS address; nothing else in the
-// kernels that use it keeps a value in M0.
+// kernels that use it keeps a value in M0. The load may follow the write of M0 after one wait
+// state (s_nop 0), which the compiler's hazard pass does not put into assembly.
 __device__ __forceinline__ void dma16(const void* g, lds_void* lds) {
   const unsigned a = static_cast<unsigned>(reinterpret_cast<__UINTPTR_TYPE__>(lds));
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(a) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(a) : "memory", "m0");
 }
 
 // The same from a wave-uniform base and a 32-bit byte offset per lane.
@@ -169,7 +170,7 @@ __device__ __forceinline__ void dma16_base(const void* base, unsigned off, lds_v
   const unsigned long long u =
       static_cast<unsigned long long>(__builtin_amdgcn_readfirstlane(static_cast<unsigned>(b >> 32))) << 32 |
       static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<unsigned>(b)));
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(u), "s"(a) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(u), "s"(a) : "memory", "m0");
 }
 
 }  // namespace dn

@@ -56,11 +56,12 @@ __device__ __forceinline__ GlobalBytes uniform(const void* q) {
 }
 
 // 16 bytes per lane global -> LDS (lane i writes lds + 16 i) from a wave-uniform base and a byte offset per
-// lane; see dma16 (common.h) for why this is assembly. dma16_if: where `on` (wave-uniform), else nothing: with an
-// empty execution mask rather than a branch, which would end the basic block (the compiler then sinks the
-// matrix instructions before it past it).
+// lane; see dma16 (common.h) for why this is assembly, with a wait state after the write of M0. dma16_if: where
+// `on` (wave-uniform), else nothing: with an empty execution mask rather than a branch, which would end the basic
+// block (the compiler then sinks the matrix instructions before it past it).
 __device__ __forceinline__ void dma16_to(GlobalBytes base, unsigned off, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds))
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base),
+               "s"(__builtin_amdgcn_readfirstlane(lds))
                : "memory", "m0");
 }
 __device__ __forceinline__ void dma16_if(bool on, GlobalBytes base, unsigned off, unsigned lds) {
