@@ -16,6 +16,7 @@
 // loop keeps the matrix cores 75 to 88 % busy; a tile's start (3.5 to 8 thousand cycles) and its stores and GELUs
 // (4 to 8) are what bounds the rest.
 #include <algorithm>
+#include <limits>
 #include <type_traits>
 
 #include "lane_swap.h"
@@ -638,12 +639,19 @@ __global__ __launch_bounds__(64 * NW) void gemm_mx4_rows_kernel(GemmMx4Params p,
   }
 }
 
+// A launch has less than 2^32 threads.
+bool fits(long long groups, int threads) { return groups * threads <= 0xffffffffll; }
+unsigned grid_of(long long groups, int threads) {
+  DN_CHECK(fits(groups, threads), "gemm_mx4: too many tiles for one launch");
+  return static_cast<unsigned>(groups);
+}
+
 template <int FM, int FN, int S, int NW, bool GE> void launch_tile(const GemmMx4Params& p, hipStream_t s) {
   static_assert(S * stage_bytes<FM>() + scale_lds(32 * FM, kScaleK) <= 64 * 1024, "no attribute needed, two workgroups per CU");
   const size_t lds = tile_lds<FM, S>(p.K);
   const int mt = ceil_div(p.M, 32 * FM), nt = ceil_div(p.N, 32 * FN * NW);
-  DN_CHECK((long long)mt * nt <= 0x7fffffffll, "gemm_mx4: too many tiles");
-  hipLaunchKernelGGL((gemm_mx4_kernel<FM, FN, S, NW, GE>), dim3(mt * nt), dim3(64 * NW), lds, s, p, mt, nt);
+  const unsigned grid = grid_of((long long)mt * nt, 64 * NW);
+  hipLaunchKernelGGL((gemm_mx4_kernel<FM, FN, S, NW, GE>), dim3(grid), dim3(64 * NW), lds, s, p, mt, nt);
 }
 
 // GEGLU with the last `small` column bands in tiles of 64 rows.
@@ -652,16 +660,15 @@ void launch_geglu(const GemmMx4Params& p, int small, hipStream_t s) {
                 "no attribute needed, two workgroups per CU");
   const size_t lds = std::max(tile_lds<4, 3>(p.K), tile_lds<2, 4>(p.K));
   const int mt = ceil_div(p.M, 128), mt2 = ceil_div(p.M, 64), nt = ceil_div(p.N, 256) - small;
-  const long long grid = (long long)mt * nt + (long long)mt2 * small;
-  DN_CHECK(grid <= 0x7fffffffll, "gemm_mx4: too many tiles");
-  hipLaunchKernelGGL(gemm_mx4_geglu_kernel, dim3((unsigned)grid), dim3(256), lds, s, p, mt, nt, mt2);
+  const unsigned grid = grid_of((long long)mt * nt + (long long)mt2 * small, 256);
+  hipLaunchKernelGGL(gemm_mx4_geglu_kernel, dim3(grid), dim3(256), lds, s, p, mt, nt, mt2);
 }
 
 template <bool GE> void launch_rows(const GemmMx4Params& p, hipStream_t s) {
   constexpr int NW = 8;
   const int nt = p.N / (GE ? 64 : 32), mt = ceil_div(p.M, 32);
-  DN_CHECK((long long)mt * nt <= 0x7fffffffll, "gemm_mx4: too many tiles");
-  hipLaunchKernelGGL((gemm_mx4_rows_kernel<NW, GE>), dim3(mt * nt), dim3(64 * NW), 0, s, p, nt);
+  const unsigned grid = grid_of((long long)mt * nt, 64 * NW);
+  hipLaunchKernelGGL((gemm_mx4_rows_kernel<NW, GE>), dim3(grid), dim3(64 * NW), 0, s, p, nt);
 }
 
 }  // namespace
@@ -676,6 +683,8 @@ void gemm_mx4_check(const GemmMx4Params& p) {
   DN_CHECK(gemm_mx4_layout(p.N, p.K) && p.M >= 1, "gemm_mx4: N % 32 == 0 and K % 128 == 0 needed");
   DN_CHECK(p.a && p.b && p.out, "gemm_mx4: null operand");
   DN_CHECK(p.N <= kMaxDim && p.K <= kMaxDim, "gemm_mx4: N and K at most 2^22");
+  // the largest tiles have to fit a launch; M is then at most 2^31 - 128, and no row number of a tile overflows
+  DN_CHECK(fits((long long)ceil_div(p.M, 128) * ceil_div(p.N, 256), 256), "gemm_mx4: too many tiles for one launch");
   DN_CHECK(!p.geglu || (p.N % 64 == 0 && !p.resid), "gemm_mx4: GEGLU takes value / gate pairs of 64 columns, no residual");
   DN_CHECK(((uintptr_t)p.a | (uintptr_t)p.b) % 16 == 0 && (uintptr_t)p.bias % 4 == 0, "gemm_mx4: operands must be 16-byte aligned");
   DN_CHECK((uintptr_t)p.out % (p.out_f32 ? 4 : p.geglu ? 16 : 2) == 0 && (uintptr_t)p.resid % (p.resid_f32 ? 4 : 2) == 0,
@@ -689,48 +698,59 @@ namespace {
 // instructions do, a workgroup alone (`one`) somewhat more than half of it, as waits are not covered; `fixed`
 // is a tile's start and end. The constants are fitted to measured times of 20 shapes, M 100 .. 32768, N 160 ..
 // 5120, K 640 .. 5120.
-float tile_cost(const GemmMx4Params& p, int cus, int bm, int bn, float one, float two, float fixed) {
-  const long long tiles = (long long)ceil_div(p.M, bm) * ceil_div(p.N, bn), per_cu = (tiles + cus - 1) / cus;
-  return p.K / kStageK * (one * (per_cu % 2) + two * (per_cu / 2)) + fixed * per_cu;
+// A shape whose tiles do not fit a launch costs more than any other.
+float tile_cost(int M, int N, int K, int cus, int bm, int bn, int threads, float one, float two, float fixed) {
+  const long long tiles = (long long)ceil_div(M, bm) * ceil_div(N, bn), per_cu = (tiles + cus - 1) / cus;
+  if (!fits(tiles, threads)) return std::numeric_limits<float>::max();
+  return K / kStageK * (one * (per_cu % 2) + two * (per_cu / 2)) + fixed * per_cu;
 }
 
 }  // namespace
 
-void gemm_mx4(const GemmMx4Params& p, int cus, hipStream_t s) {
-  gemm_mx4_check(p);
+Mx4Plan gemm_mx4_plan(int M, int N, int K, bool geglu, int cus) {
   // Two rows kernel workgroups of 8 waves per CU: as long as all of its 32 x 32 blocks are resident at once, it
   // wins, since no tile fills the chip then (200 x 1280, K = 5120: 9.4 us, the 64 x 128 tiles 11.0; 77 x 5120
   // GEGLU, K = 1280: 5.8 and 8.6); with more it loses to re-reading B per 32 rows (128 x 5120, K = 2560: 8.4
   // and 6.2).
-  if ((long long)ceil_div(p.M, 32) * (p.N / (p.geglu ? 64 : 32)) <= 2ll * cus) {
-    p.geglu ? launch_rows<true>(p, s) : launch_rows<false>(p, s);
-  } else if (p.geglu) {
+  const int pair = geglu ? 64 : 32;
+  if ((long long)ceil_div(M, 32) * (N / pair) <= 2ll * cus) return Mx4Plan{32, pair, 0};
+  if (geglu) {
     // 64-row tiles while all of them run at once, each on a CU of its own (300 x 2560, K = 640: 5.6 us, 128 rows
     // 7.2); with more, 128 rows are faster (8192 x 2560, K = 640: 33.7 and 29.0). After whole rounds of two tiles
     // per CU, a last one of half the CUs or fewer runs as 64-row tiles on twice as many (2048 x 5120, K = 1280:
     // 24.8 and 22.4 us; with all CUs in it there is nothing to gain: 8192 x 2560, K = 640: 28.8 and 29.5)
-    const int mt = ceil_div(p.M, 128), nt = ceil_div(p.N, 256);
+    const int mt = ceil_div(M, 128), nt = ceil_div(N, 256);
     const long long tiles = (long long)mt * nt, tail = tiles % (2 * cus);
     int small = 0;
-    if ((long long)ceil_div(p.M, 64) * nt <= cus)
+    if ((long long)ceil_div(M, 64) * nt <= cus)
       small = nt;
     else if (2 * tail <= cus)
       small = (int)((tail + mt - 1) / mt);
-    launch_geglu(p, small, s);
-  } else {
-    // 128 x 256 does most work per byte from LDS and L2 (4096^3 39.8 us, 64 x 128 58, 64 x 160 68); the smaller
-    // ones win where they even out the tiles per CU (2048 x 1280, K = 5120: 24.5, 19.8, 15.0; 700 x 1280,
-    // K = 2560: 16.0, 8.4, 9.2)
-    const float big = tile_cost(p, cus, 128, 256, 0.43f, 0.86f, 4.2f);
-    const float small = tile_cost(p, cus, 64, 128, 0.18f, 0.39f, 1.2f);
-    const float five = tile_cost(p, cus, 64, 160, 0.21f, 0.48f, 2.5f);
-    if (big <= small && big <= five)
-      launch_tile<4, 2, 3, 4, false>(p, s);
-    else if (small <= five)
-      launch_tile<2, 1, 4, 4, false>(p, s);
-    else
-      launch_tile<2, 1, 4, 5, false>(p, s);
+    return Mx4Plan{128, 256, small};
   }
+  // 128 x 256 does most work per byte from LDS and L2 (4096^3 39.8 us, 64 x 128 58, 64 x 160 68); the smaller
+  // ones win where they even out the tiles per CU (2048 x 1280, K = 5120: 24.5, 19.8, 15.0; 700 x 1280,
+  // K = 2560: 16.0, 8.4, 9.2)
+  const float big = tile_cost(M, N, K, cus, 128, 256, 256, 0.43f, 0.86f, 4.2f);
+  const float small = tile_cost(M, N, K, cus, 64, 128, 256, 0.18f, 0.39f, 1.2f);
+  const float five = tile_cost(M, N, K, cus, 64, 160, 320, 0.21f, 0.48f, 2.5f);
+  if (big <= small && big <= five) return Mx4Plan{128, 256, 0};
+  return small <= five ? Mx4Plan{64, 128, 0} : Mx4Plan{64, 160, 0};
+}
+
+void gemm_mx4(const GemmMx4Params& p, int cus, hipStream_t s) {
+  gemm_mx4_check(p);
+  const Mx4Plan g = gemm_mx4_plan(p.M, p.N, p.K, p.geglu != 0, cus);
+  if (g.bm == 32)
+    p.geglu ? launch_rows<true>(p, s) : launch_rows<false>(p, s);
+  else if (p.geglu)
+    launch_geglu(p, g.small, s);
+  else if (g.bm == 128)
+    launch_tile<4, 2, 3, 4, false>(p, s);
+  else if (g.bn == 128)
+    launch_tile<2, 1, 4, 4, false>(p, s);
+  else
+    launch_tile<2, 1, 4, 5, false>(p, s);
   DN_HIP(hipGetLastError());
 }
 

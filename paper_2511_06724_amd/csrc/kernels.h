@@ -235,6 +235,12 @@ struct GemmMx4Params {
 bool gemm_mx4_layout(int N, int K);
 size_t gemm_mx4_code_bytes(int N, int K);
 size_t gemm_mx4_bytes(int N, int K);  // codes and scales of a packed matrix
+// What a product of these sizes runs as: tiles of bm x bn columns of w (bm = 32: the kernel of few rows), `small` of
+// a GEGLU's column bands as 64-row tiles.
+struct Mx4Plan {
+  int bm = 0, bn = 0, small = 0;
+};
+Mx4Plan gemm_mx4_plan(int M, int N, int K, bool geglu, int cus);
 void gemm_mx4_check(const GemmMx4Params& p);  // throws for what gemm_mx4 does not take
 void gemm_mx4(const GemmMx4Params& p, int cus, hipStream_t s);
 
