@@ -717,15 +717,17 @@ Mx4Plan gemm_mx4_plan(int M, int N, int K, bool geglu, int cus) {
   if (geglu) {
     // 64-row tiles while all of them run at once, each on a CU of its own (300 x 2560, K = 640: 5.6 us, 128 rows
     // 7.2); with more, 128 rows are faster (8192 x 2560, K = 640: 33.7 and 29.0). After whole rounds of two tiles
-    // per CU, a last one of half the CUs or fewer runs as 64-row tiles on twice as many (2048 x 5120, K = 1280:
-    // 24.8 and 22.4 us; with all CUs in it there is nothing to gain: 8192 x 2560, K = 640: 28.8 and 29.5)
-    const int mt = ceil_div(M, 128), nt = ceil_div(N, 256);
-    const long long tiles = (long long)mt * nt, tail = tiles % (2 * cus);
+    // per CU, a last one of half the CUs or fewer runs as 64-row tiles (2048 x 5120, K = 1280: 24.8 and 22.4 us; with
+    // all CUs in it there is nothing to gain: 8192 x 2560, K = 640: 28.8 and 29.5), as whole column bands: also where
+    // a band is longer than that round (33024 x 256, K = 640: 15.6 and 15.0 us), unless that takes in every band
+    // (65664 x 128, K = 640: 15.8 and 17.0) or more tiles than a launch holds.
+    const int mt = ceil_div(M, 128), mt2 = ceil_div(M, 64), nt = ceil_div(N, 256);
+    const long long tail = (long long)mt * nt % (2 * cus), bands = (tail + mt - 1) / mt;
     int small = 0;
-    if ((long long)ceil_div(M, 64) * nt <= cus)
+    if ((long long)mt2 * nt <= cus)
       small = nt;
-    else if (2 * tail <= cus)
-      small = (int)((tail + mt - 1) / mt);
+    else if (2 * tail <= cus && bands < nt && fits(mt * (nt - bands) + mt2 * bands, 256))
+      small = (int)bands;
     return Mx4Plan{128, 256, small};
   }
   // 128 x 256 does most work per byte from LDS and L2 (4096^3 39.8 us, 64 x 128 58, 64 x 160 68); the smaller

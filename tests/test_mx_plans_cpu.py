@@ -44,7 +44,7 @@ def test_geglu_plans_are_the_measured_best(M, N, K, want, us, other):
     assert plan(M, N, K, geglu=True) == want, f"{us} us wanted, {other}"
 
 
-@pytest.mark.parametrize("geglu", [False])
+@pytest.mark.parametrize("geglu", [False, True])
 def test_plans_fit_a_launch(geglu):
     """Whatever passes the checks of the call is given tiles that one launch holds."""
     for M in (1, 33, 1000, 10 ** 6, 2 ** 24, 2 ** 28 + 1, 2 ** 30, 2 ** 30 + 1, 2 ** 31 - 128):
@@ -64,3 +64,10 @@ def test_more_tiles_than_a_launch_holds_refused(M, N, K, geglu):
 def test_a_product_that_only_the_largest_tiles_hold_is_planned_with_them():
     """2^24 tiles of 64 rows are one more than a launch holds: 73 GB of x, 69 GB of bf16 y."""
     assert plan(2 ** 30, 32, 128)[:2] == (128, 256)
+
+
+def test_geglu_tiles_are_not_all_small_for_a_short_last_round():
+    for M in (65664, 10 ** 6 + 100, 2 ** 30 + 1):
+        for N in (64, 256):
+            assert plan(M, N, 640, geglu=True) == (128, 256, 0), (M, N)
+    assert plan(33024, 512, 640, geglu=True) == (128, 256, 1)
