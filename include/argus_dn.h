@@ -390,7 +390,8 @@ dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, co
  *   and 64-deep step, the lanes' 32-byte operands in 2 KB), code = round(w / scale_n),
  *   then N fp32 scales scale_n = max_k |w[n][k]| / 448 (1 for a zero row);
  *   dn_packed_weight_elems gives the total in bytes.
- * DN_MXFP4: w is fp32 [N][K] (N % 32 == 0, K % 128 == 0), quantised as the rows of dn_mx_quantize;
+ * DN_MXFP4: w is fp32 [N][K] (N % 32 == 0, K % 128 == 0, both at most 2^22, N K < 2^35), quantised as the rows of
+ *   dn_mx_quantize;
  *   `out` (16-byte aligned) receives N * K / 2 bytes of E2M1 codes in the operand order of the 32x32x64
  *   matrix-core step (per 32 rows and 64-deep step the lanes' 16 bytes in 1 KB), then the scales (per 64
  *   rows and 128 deep, four bytes a lane), then 8 KB that products may read and ignore;

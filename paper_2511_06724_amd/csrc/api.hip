@@ -544,7 +544,7 @@ dn_status dn_packed_weight_elems(int32_t dtype, int32_t N, int32_t K, int64_t* e
       return;
     }
     if (dtype == DN_MXFP4) {
-      DN_CHECK(dn::gemm_mx4_layout(N, K), "dn_packed_weight_elems: DN_MXFP4 needs N % 32 == 0, K % 128 == 0");
+      DN_CHECK(dn::gemm_mx4_layout(N, K), "dn_packed_weight_elems: DN_MXFP4 needs N % 32 == 0, K % 128 == 0, both at most 2^22");
       *elems = (int64_t)dn::gemm_mx4_bytes(N, K);
       return;
     }
@@ -557,7 +557,7 @@ dn_status dn_pack_weight(int32_t dtype, const void* w, int32_t N, int32_t K, voi
     DN_CHECK(is_dtype_op(dtype), "dn_pack_weight: bad dtype");
     DN_CHECK(w && out, "dn_pack_weight: null pointer");
     if (dtype == DN_MXFP4) {
-      DN_CHECK(dn::gemm_mx4_layout(N, K), "dn_pack_weight: DN_MXFP4 needs N % 32 == 0, K % 128 == 0");
+      DN_CHECK(dn::gemm_mx4_layout(N, K), "dn_pack_weight: DN_MXFP4 needs N % 32 == 0, K % 128 == 0, both at most 2^22");
       DN_CHECK(reinterpret_cast<uintptr_t>(out) % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 4 == 0,
                "dn_pack_weight: DN_MXFP4 needs a 16-byte aligned output and a 4-byte aligned source");
       dn::PackParams p;
@@ -603,7 +603,7 @@ dn_status dn_op_linear(int32_t dtype, const void* x, const void* w, const float*
     DN_CHECK(!(geglu && resid), "dn_op_linear: GEGLU takes no residual");
     if (dtype == DN_MXFP4) {
       DN_CHECK(N <= 0x3fffffff && dn::gemm_mx4_layout(geglu ? 2 * N : N, K),
-               "dn_op_linear: DN_MXFP4 needs N % 32 == 0 and K % 128 == 0");
+               "dn_op_linear: DN_MXFP4 needs N % 32 == 0 and K % 128 == 0, N (GEGLU: 2N) and K at most 2^22");
       dn::GemmMx4Params q;
       q.a = x;
       q.b = w;

@@ -673,16 +673,17 @@ template <bool GE> void launch_rows(const GemmMx4Params& p, hipStream_t s) {
 
 }  // namespace
 
-bool gemm_mx4_layout(int N, int K) { return N >= 32 && N % 32 == 0 && K >= kStageK && K % kStageK == 0; }
+bool gemm_mx4_layout(int N, int K) {
+  return N >= 32 && N % 32 == 0 && N <= kMaxDim && K >= kStageK && K % kStageK == 0 && K <= kMaxDim;
+}
 size_t gemm_mx4_code_bytes(int N, int K) { return (size_t)N * (K / 2); }
 size_t gemm_mx4_bytes(int N, int K) {
   return (size_t)N * (K / 2) + (size_t)((N + 63) / 64 * 64) * (K / 32) + kBSpare;
 }
 
 void gemm_mx4_check(const GemmMx4Params& p) {
-  DN_CHECK(gemm_mx4_layout(p.N, p.K) && p.M >= 1, "gemm_mx4: N % 32 == 0 and K % 128 == 0 needed");
+  DN_CHECK(gemm_mx4_layout(p.N, p.K) && p.M >= 1, "gemm_mx4: N % 32 == 0 and K % 128 == 0, both at most 2^22, needed");
   DN_CHECK(p.a && p.b && p.out, "gemm_mx4: null operand");
-  DN_CHECK(p.N <= kMaxDim && p.K <= kMaxDim, "gemm_mx4: N and K at most 2^22");
   // the largest tiles have to fit a launch; M is then at most 2^31 - 128, and no row number of a tile overflows
   DN_CHECK(fits((long long)ceil_div(p.M, 128) * ceil_div(p.N, 256), 256), "gemm_mx4: too many tiles for one launch");
   DN_CHECK(!p.geglu || (p.N % 64 == 0 && !p.resid), "gemm_mx4: GEGLU takes value / gate pairs of 64 columns, no residual");

@@ -327,8 +327,8 @@ void mx_fetch(int fmt, const void* table, long long n_slots, long long cols, con
 void pack_mx4(const PackParams& p, unsigned char* scales, hipStream_t s) {
   DN_CHECK(p.col_mode == 0 && p.rows % 32 == 0 && p.cols % 128 == 0 && p.src_cols == p.cols,
            "pack_mx4: rows must be a multiple of 32, columns of 128");
-  const long long n = (long long)p.rows * (p.cols / 8);
-  hipLaunchKernelGGL(pack_mx4_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, s, p, scales);
+  const unsigned grid = grid_for((long long)p.rows * (p.cols / 8), 256);
+  hipLaunchKernelGGL(pack_mx4_kernel, dim3(grid), dim3(256), 0, s, p, scales);
   DN_HIP(hipGetLastError());
 }
 
