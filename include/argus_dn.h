@@ -317,7 +317,8 @@ dn_status ac_fetch_latent(const uint16_t* cache_latents, int64_t n, int64_t nume
  *   written (reads go a few bytes past the last scale).
  * An MX buffer of n rows is also a cache of n slots: a latent table (cols = latent_c*H*W) or an
  * embedding table (cols = dim). All calls below are asynchronous on `stream`, allocate nothing and
- * keep no state, so calls on different buffers may overlap and be captured into graphs.
+ * keep no state, so calls on different buffers may overlap and be captured into graphs. Buffers for which
+ * nothing else is said are aligned to their elements (slots and indices: 8 bytes).
  * ------------------------------------------------------------------------- */
 
 /* Bytes of an MX buffer of `rows` x `cols` values, 1 <= cols <= 2^31 - 32. */

@@ -195,6 +195,9 @@ bool is_mx(int32_t d) { return d == DN_MXFP4 || d == DN_MXFP8; }
 bool is_dtype_op(int32_t d) { return is_dtype8(d) || d == DN_MXFP4; }  // operand types of the dense layers and LayerNorm
 static_assert(DN_MXFP4 == dn::kMx4 && DN_MXFP8 == dn::kMx8, "the kernels' format numbers");
 
+// Whether `p` (which may be null) is aligned to its elements of n bytes.
+bool on(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
 // Arguments the MX row calls share: a table of n_slots rows of `cols` values, `rows` rows in fp32 / bf16 /
 // fp16 (dense rows ld apart) on the other side.
 void check_mx(const char* who, int32_t dtype, const void* table, int64_t n_slots, int64_t cols, const void* x, int64_t ld,
@@ -479,6 +482,7 @@ dn_status dn_mx_quantize(int32_t dtype, int32_t x_dtype, const void* x, int64_t 
 dn_status dn_mx_dequantize(int32_t dtype, const void* q, int64_t rows, int64_t cols, float* y, int64_t ldy, void* stream) {
   return guarded([&] {
     check_mx("dn_mx_dequantize", dtype, q, rows, cols, y, ldy, rows);
+    DN_CHECK(on(y, 4), "dn_mx_dequantize: misaligned output");
     dn::mx_fetch(dtype, q, rows, cols, nullptr, rows, y, ldy, as_stream(stream));
   });
 }
@@ -486,7 +490,8 @@ dn_status dn_mx_dequantize(int32_t dtype, const void* q, int64_t rows, int64_t c
 dn_status ac_mx_store_bytes(int64_t n_rows, int64_t n_slots, int64_t* bytes) {
   return guarded([&] {
     DN_CHECK(bytes, "ac_mx_store_bytes: null pointer");
-    DN_CHECK(n_rows >= 1 && n_slots >= 1, "ac_mx_store_bytes: bad sizes");
+    // as many slots as a table can have (dn_mx_bytes)
+    DN_CHECK(n_rows >= 1 && n_slots >= 1 && n_slots <= (1ll << 46), "ac_mx_store_bytes: bad sizes");
     *bytes = static_cast<int64_t>(dn::mx_store_workspace(n_rows, n_slots));
   });
 }
@@ -495,7 +500,7 @@ dn_status ac_mx_store(int32_t dtype, int32_t x_dtype, const void* x, int64_t ldx
                       void* table, int64_t n_slots, int64_t dim, void* ws, void* stream) {
   return guarded([&] {
     check_mx("ac_mx_store", dtype, table, n_slots, dim, x, ldx, n_rows);
-    DN_CHECK(slots, "ac_mx_store: null slots");
+    DN_CHECK(slots && on(slots, 8), "ac_mx_store: null or misaligned slots");
     DN_CHECK((ws && reinterpret_cast<uintptr_t>(ws) % 4 == 0) || dn::mx_store_workspace(n_rows, n_slots) == 0,
              "ac_mx_store: this many rows need the workspace of ac_mx_store_bytes");
     store_rows("ac_mx_store", dtype, x_dtype, x, ldx, n_rows, dim, slots, n_slots, table, ws, stream);
@@ -506,7 +511,8 @@ dn_status ac_mx_fetch(int32_t dtype, const void* table, int64_t n_slots, int64_t
                       float* out, int64_t ldo, void* stream) {
   return guarded([&] {
     check_mx("ac_mx_fetch", dtype, table, n_slots, dim, out, ldo, n_idx);
-    DN_CHECK(idx, "ac_mx_fetch: null indices");
+    DN_CHECK(idx && on(idx, 8), "ac_mx_fetch: null or misaligned indices");
+    DN_CHECK(on(out, 4), "ac_mx_fetch: misaligned output");
     dn::mx_fetch(dtype, table, n_slots, dim, reinterpret_cast<const long long*>(idx), n_idx, out, ldo, as_stream(stream));
   });
 }
@@ -525,7 +531,8 @@ dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, co
     check_mx("ac_mx_lookup", dtype, table, n, dim, query_embs, dim, nq);
     DN_CHECK(out_idx && ws, "ac_mx_lookup: null pointer");
     DN_CHECK((levels != nullptr) == (out_k != nullptr), "ac_mx_lookup: a level table and a level output go together");
-    DN_CHECK(reinterpret_cast<uintptr_t>(ws) % 16 == 0, "ac_mx_lookup: the workspace must be 16-byte aligned");
+    DN_CHECK(on(ws, 16), "ac_mx_lookup: the workspace must be 16-byte aligned");
+    DN_CHECK(on(query_embs, 2) && on(out_idx, 8) && on(out_score, 4) && on(out_k, 4), "ac_mx_lookup: misaligned queries or outputs");
     dn::KTable kt;
     if (levels) kt = k_table(levels);
     dn::mx_lookup(dtype, query_embs, nq, table, n, dim, ws, reinterpret_cast<long long*>(out_idx), out_score,

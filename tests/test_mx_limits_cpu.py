@@ -17,3 +17,29 @@ def test_weights_past_the_products_limits_are_not_packed(N, K, msg):
     if msg == b"2^22":
         n = C.c_int64(-7)
         assert dn.lib.dn_packed_weight_elems(dn.DN_MXFP4, N, K, C.byref(n)) == dn.DN_EINVAL and n.value == -7
+
+
+@pytest.mark.parametrize("off", [1, 2, 4])
+def test_buffers_off_their_elements_refused(off):
+    """Every buffer of the row calls is aligned to its elements: fp32 rows 4 bytes, slots and indices 8."""
+    f = dn.DN_MXFP4
+    calls = [lambda: dn.lib.ac_mx_store(f, dn.DN_FP32, P, 64, 4, P + off, P, 9, 64, None, None),
+             lambda: dn.lib.ac_mx_fetch(f, P, 9, 64, P + off, 4, P, 64, None),
+             lambda: dn.lib.ac_mx_lookup(f, P, 3, P, 9, 64, None, P + off, P, None, P, None)]
+    if off < 4:
+        tab = C.byref(dn.k_table([0.5], [1, 2]))
+        calls += [lambda: dn.lib.dn_mx_dequantize(f, P, 4, 64, P + off, 64, None),
+                  lambda: dn.lib.ac_mx_fetch(f, P, 9, 64, P, 4, P + off, 64, None),
+                  lambda: dn.lib.ac_mx_lookup(f, P, 3, P, 9, 64, None, P, P + off, None, P, None),
+                  lambda: dn.lib.ac_mx_lookup(f, P, 3, P, 9, 64, tab, P, P, P + off, P, None)]
+    if off < 2:
+        calls += [lambda: dn.lib.ac_mx_lookup(f, P + off, 3, P, 9, 64, None, P, P, None, P, None)]
+    for call in calls:
+        assert call() == dn.DN_EINVAL
+        assert b"misaligned" in dn.lib.dn_last_error()
+
+
+def test_store_workspace_of_more_slots_than_a_table_has_refused():
+    n = C.c_int64(-7)
+    assert dn.lib.ac_mx_store_bytes(1000, 2 ** 62, C.byref(n)) == dn.DN_EINVAL and n.value == -7
+    assert dn.lib.ac_mx_store_bytes(1000, 2 ** 46, C.byref(n)) == dn.DN_OK and n.value == 2 ** 48
