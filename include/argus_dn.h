@@ -318,7 +318,8 @@ dn_status ac_fetch_latent(const uint16_t* cache_latents, int64_t n, int64_t nume
  * An MX buffer of n rows is also a cache of n slots: a latent table (cols = latent_c*H*W) or an
  * embedding table (cols = dim). All calls below are asynchronous on `stream`, allocate nothing and
  * keep no state, so calls on different buffers may overlap and be captured into graphs. Buffers for which
- * nothing else is said are aligned to their elements (slots and indices: 8 bytes).
+ * nothing else is said are aligned to their elements (slots and indices: 8 bytes). A call that quantises or
+ * reads rows takes at most 2^36 - 4096 values (whole blocks counted).
  * ------------------------------------------------------------------------- */
 
 /* Bytes of an MX buffer of `rows` x `cols` values, 1 <= cols <= 2^31 - 32. */
@@ -357,8 +358,8 @@ dn_status ac_mx_fetch(int32_t dtype, const void* table, int64_t n_slots, int64_t
  * retrieved); out_score device float [nq] or NULL (0 where the index is -1); levels (host, read during
  * the call) and out_k (device int32 [nq]) are both given, or both NULL: the approximation level as in
  * ac_lookup_batch_k. ws: device, 16-byte aligned, ac_mx_lookup_bytes bytes, contents arbitrary;
- * overlapping calls need workspaces of their own. Any nq >= 1, n >= 1, 1 <= dim <= 16384; up to dim
- * 1024 the table is read once per 64 queries. */
+ * overlapping calls need workspaces of their own. Any nq >= 1, n >= 1, 1 <= dim <= 16384. The table is read once
+ * per 64 queries for 8 <= dim <= 768, once per 32 up to 1024, and else once per two (over 8192: one). */
 dn_status ac_mx_lookup_bytes(int32_t nq, int64_t n, int32_t dim, int64_t* bytes);
 dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, const void* table, int64_t n,
                        int32_t dim, const ac_k_table* levels, int64_t* out_idx, float* out_score, int32_t* out_k,

@@ -5,13 +5,13 @@
 // no sum over- or underflows for any scales. A zero row, or one with a NaN block, never wins; ties go to
 // the lowest row at every stage.
 //
-// Rows of 8 .. 1024 values (mx_scan_mfma_kernel): codes converted to fp16 (exact) against up to 64 queries
-// held in registers, on the matrix cores; the table is read once per pass, 17/32 (33/32) bytes a value.
+// Rows of 8 .. 1024 values (mx_scan_mfma_kernel): codes converted to fp16 (exact) against up to 64 queries (32 past
+// 768 values) held in registers, on the matrix cores; the table is read once per pass, 17/32 (33/32) bytes a value.
 // Bound by that for few queries: 100000 x 768 E2M1 rows (41 MB) 13.1 us with the reduction for one query (one
 // pass at 5.1 TB/s: 8.0), 13.9 for 16; a million rows 73.4 (79.7). For 64 queries 21.8: a third of it the
 // queries' way into the registers of every CU (98 KB each), the rest products and conversions (16 cycles per
 // product, 8 per conversion of two values).
-// Other rows (mx_scan_kernel): one or two queries per pass, packed dot products in fp32.
+// Other rows (mx_scan_kernel): two queries per pass (one past 8192 values), packed dot products in fp32.
 #include <algorithm>
 #include <type_traits>
 
