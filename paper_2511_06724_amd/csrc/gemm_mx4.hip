@@ -535,10 +535,10 @@ __device__ __forceinline__ int xcd_unit(int wg, int units) {
   return xcd * (units / kXcds) + min(xcd, units % kXcds) + idx;
 }
 
-template <int FM, int FN, int S, int NW, bool GE>
+template <int FM, int FN, int S, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_mx4_kernel(GemmMx4Params p, int mt, int nt) {
   const int u = xcd_unit(blockIdx.x, mt * nt);
-  mx4_tile<FM, FN, S, NW, GE>(p, (u % mt) * 32 * FM, (u / mt) * 32 * FN * NW);
+  mx4_tile<FM, FN, S, NW, false>(p, (u % mt) * 32 * FM, (u / mt) * 32 * FN * NW);
 }
 
 // GEGLU: the first nt column bands in mt tiles of 128 rows, then bands in mt2 tiles of 64 rows.
@@ -646,12 +646,12 @@ unsigned grid_of(long long groups, int threads) {
   return static_cast<unsigned>(groups);
 }
 
-template <int FM, int FN, int S, int NW, bool GE> void launch_tile(const GemmMx4Params& p, hipStream_t s) {
+template <int FM, int FN, int S, int NW> void launch_tile(const GemmMx4Params& p, hipStream_t s) {
   static_assert(S * stage_bytes<FM>() + scale_lds(32 * FM, kScaleK) <= 64 * 1024, "no attribute needed, two workgroups per CU");
   const size_t lds = tile_lds<FM, S>(p.K);
   const int mt = ceil_div(p.M, 32 * FM), nt = ceil_div(p.N, 32 * FN * NW);
   const unsigned grid = grid_of((long long)mt * nt, 64 * NW);
-  hipLaunchKernelGGL((gemm_mx4_kernel<FM, FN, S, NW, GE>), dim3(grid), dim3(64 * NW), lds, s, p, mt, nt);
+  hipLaunchKernelGGL((gemm_mx4_kernel<FM, FN, S, NW>), dim3(grid), dim3(64 * NW), lds, s, p, mt, nt);
 }
 
 // GEGLU with the last `small` column bands in tiles of 64 rows.
@@ -749,11 +749,11 @@ void gemm_mx4(const GemmMx4Params& p, int cus, hipStream_t s) {
   else if (p.geglu)
     launch_geglu(p, g.small, s);
   else if (g.bm == 128)
-    launch_tile<4, 2, 3, 4, false>(p, s);
+    launch_tile<4, 2, 3, 4>(p, s);
   else if (g.bn == 128)
-    launch_tile<2, 1, 4, 4, false>(p, s);
+    launch_tile<2, 1, 4, 4>(p, s);
   else
-    launch_tile<2, 1, 4, 5, false>(p, s);
+    launch_tile<2, 1, 4, 5>(p, s);
   DN_HIP(hipGetLastError());
 }
 

@@ -489,14 +489,6 @@ template <> struct Store4<float> {
   }
 };
 
-// One wave per row. With NS > 0 the row is first rebuilt from the residual stream:
-// x[row] = (resid ? x[row] : 0) + bias + sum_s part[s][row] in that order (the reduction of
-// a split-K GEMM that wrote fp32 partial slabs), and written back; then
-// y = (x - mean) * rstd * gamma + beta with two-pass mean / variance. Every load of the
-// row (x, the slabs, the bias; gamma and beta too when NS = 0) is issued before the first
-// use, so a row waits on one memory latency; the two wave sums use DPP lane moves;
-// vector columns past C are skipped wave-uniformly, lanes past C read a valid column and
-// are masked.
 // Four values of a row of an MX4 buffer [M][C], lanes of eight a block: y the row's codes, sc its scales.
 __device__ __forceinline__ void st4_mx(uint8_t* y, uint8_t* sc, int i, float a, float b, float c, float d) {
   const float v[8] = {a, b, c, d, 0.f, 0.f, 0.f, 0.f};
@@ -505,6 +497,14 @@ __device__ __forceinline__ void st4_mx(uint8_t* y, uint8_t* sc, int i, float a, 
   if ((i & 7) == 0) sc[i / 8] = static_cast<uint8_t>(s);
 }
 
+// One wave per row. With NS > 0 the row is first rebuilt from the residual stream:
+// x[row] = (resid ? x[row] : 0) + bias + sum_s part[s][row] in that order (the reduction of
+// a split-K GEMM that wrote fp32 partial slabs), and written back; then
+// y = (x - mean) * rstd * gamma + beta with two-pass mean / variance. Every load of the
+// row (x, the slabs, the bias; gamma and beta too when NS = 0) is issued before the first
+// use, so a row waits on one memory latency; the two wave sums use DPP lane moves;
+// vector columns past C are skipped wave-uniformly, lanes past C read a valid column and
+// are masked.
 // T = Mx4Row: y is an MX4 buffer (C % 32 == 0, so the eight lanes of a block are active together).
 template <typename T, int NS>
 __global__ __launch_bounds__(256) void ln_kernel(float* x, T* y, long long M, int C, const float* gamma,
