@@ -474,7 +474,7 @@ dn_status dn_op_groupnorm(int32_t dtype, const void* x, void* y, int32_t n, int3
 
 /* LayerNorm over the last axis: x fp32 [M][C] (the residual stream), y [M][C]
  * in `dtype` (E4M3 codes for DN_FP8, nearest even, saturating; an MX buffer of M rows of C
- * values for DN_MXFP4, C % 32 == 0); C a multiple of 4, at most 2048. Asynchronous. */
+ * values for DN_MXFP4, C % 32 == 0); C a multiple of 4, at most 2048; M at most 2^26 - 4. Asynchronous. */
 dn_status dn_op_layernorm(int32_t dtype, const float* x, void* y, int64_t M, int32_t C, const float* gamma,
                           const float* beta, float eps, void* stream);
 

@@ -668,6 +668,7 @@ template <typename T>
 void layernorm_reduce(float* x, T* y, long long M, int C, const float* gamma, const float* beta, float eps,
                       const float* part, int nsplit, const float* bias, bool resid, hipStream_t s) {
   DN_CHECK(M >= 1 && C >= 4 && C % 4 == 0 && C <= 4 * 64 * kLnMaxVec, "layernorm: C must be a multiple of 4, <= 2048");
+  DN_CHECK(M <= (1ll << 26) - 4, "layernorm: too many rows for one launch");  // of less than 2^32 threads, 64 a row
   DN_CHECK(x && y && gamma && beta, "layernorm: null");
   DN_CHECK(((uintptr_t)x | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)part | (uintptr_t)bias) % 16 == 0 &&
                (uintptr_t)y % (std::is_same<T, Mx4Row>::value ? 16 : 4 * sizeof(T)) == 0,

@@ -43,3 +43,10 @@ def test_store_workspace_of_more_slots_than_a_table_has_refused():
     n = C.c_int64(-7)
     assert dn.lib.ac_mx_store_bytes(1000, 2 ** 62, C.byref(n)) == dn.DN_EINVAL and n.value == -7
     assert dn.lib.ac_mx_store_bytes(1000, 2 ** 46, C.byref(n)) == dn.DN_OK and n.value == 2 ** 48
+
+
+@pytest.mark.parametrize("dtype", [dn.DN_FP32, dn.DN_BF16, dn.DN_FP8, dn.DN_MXFP4])
+@pytest.mark.parametrize("M", [2 ** 26 - 3, 2 ** 40])
+def test_more_rows_than_a_layernorm_launch_has_refused(dtype, M):
+    assert dn.lib.dn_op_layernorm(dtype, P, P, M, 32, P, P, 1e-5, None) == dn.DN_EINVAL
+    assert b"one launch" in dn.lib.dn_last_error()
