@@ -408,6 +408,12 @@ def _int64():
     return torch.int64
 
 
+@functools.lru_cache(maxsize=None)
+def _lookup_types():
+    import torch
+    return torch.int64, torch.float32, torch.int32
+
+
 def _rows(x, name):
     """(dtype, row stride, rows, columns) of a row source: a 2-D tensor whose rows are dense."""
     if x.dim() != 2:
@@ -510,9 +516,9 @@ def ac_mx_lookup(dtype, queries, table, n, ws, out_idx, out_score=None, out_k=No
     _buffer(table, mx_bytes(dtype, n, dim), "ac_mx_lookup")
     _buffer(ws, ac_mx_lookup_bytes(nq, n, dim), "ac_mx_lookup workspace")
     _index(out_idx, "ac_mx_lookup")
-    for t, size, name in ((out_idx, 8, "out_idx"), (out_score, 4, "out_score"), (out_k, 4, "out_k")):
-        if t is not None and (t.numel() < nq or t.element_size() != size or not t.is_contiguous()):
-            raise ValueError(f"ac_mx_lookup: {name} must be dense with one entry per query")
+    for t, kind, name in zip((out_idx, out_score, out_k), _lookup_types(), ("out_idx", "out_score", "out_k")):
+        if t is not None and (t.numel() < nq or t.dtype is not kind or not t.is_contiguous()):
+            raise ValueError(f"ac_mx_lookup: {name} must be dense with one {kind} per query")
     tab = None
     if thresholds is not None:
         if levels is None or len(thresholds) >= AC_MAX_K_LEVELS or len(levels) != len(thresholds) + 1:

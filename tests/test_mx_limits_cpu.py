@@ -50,3 +50,13 @@ def test_store_workspace_of_more_slots_than_a_table_has_refused():
 def test_more_rows_than_a_layernorm_launch_has_refused(dtype, M):
     assert dn.lib.dn_op_layernorm(dtype, P, P, M, 32, P, P, 1e-5, None) == dn.DN_EINVAL
     assert b"one launch" in dn.lib.dn_last_error()
+
+
+@pytest.mark.parametrize("change", [dict(score="float64"), dict(score="int32"), dict(k="float32"), dict(k="int64"), dict(idx="float64")])
+def test_lookup_outputs_of_another_type_refused(change):
+    import torch
+    t = {**dict(idx="int64", score="float32", k="int32"), **change}
+    out = [torch.zeros(4, dtype=getattr(torch, t[n])) for n in ("idx", "score", "k")]
+    table, ws = (torch.zeros(n, dtype=torch.uint8) for n in (dn.mx_bytes(dn.DN_MXFP4, 9, 64), dn.ac_mx_lookup_bytes(4, 9, 64)))
+    with pytest.raises(ValueError):
+        dn.ac_mx_lookup(dn.DN_MXFP4, torch.zeros(4, 64, dtype=torch.float16), table, 9, ws, *out, [0.5], [1, 2], stream=0)
