@@ -456,7 +456,7 @@ def mx_dequantize(dtype, q, rows, cols, y=None, stream=None):
     import torch
     _buffer(q, mx_bytes(dtype, rows, cols), "mx_dequantize")
     if y is None:
-        y = torch.empty(rows, cols, device=q.device)
+        y = torch.empty(rows, cols, device=q.device, dtype=torch.float32)
     yt, ldy, r, c = _rows(y, "mx_dequantize")
     if yt != DN_FP32 or (r, c) != (rows, cols):
         raise ValueError("mx_dequantize: y must be float32 [rows, cols]")

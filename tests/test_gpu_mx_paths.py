@@ -33,6 +33,19 @@ def _nan_blocks(q, M, N):
     return nan
 
 
+def test_dequantize_allocates_fp32_whatever_the_default_type():
+    announce("mx_dequantize under another default type")
+    x = torch.randn(5, 70, device=DEV)
+    q = dn.mx_quantize(dn.DN_MXFP8, x)
+    want = dn.mx_dequantize(dn.DN_MXFP8, q, 5, 70)
+    torch.set_default_dtype(torch.float64)
+    try:
+        got = dn.mx_dequantize(dn.DN_MXFP8, q, 5, 70)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert got.dtype is torch.float32 and torch.equal(got, want)
+
+
 # ----------------------------------------------------------------------------- NaN and infinities
 
 @pytest.mark.parametrize("shape,tile", [((201, 96, 256), ROWS), ((700, 1280, 256), SMALL), ((2048, 1280, 256), FIVE), ((2000, 1248, 896), FIVE),
