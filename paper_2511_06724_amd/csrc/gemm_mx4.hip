@@ -10,11 +10,12 @@
 //    that sixteen consecutive rows' reads of a chunk touch all banks. The scales are copied once;
 //  - C^T = B A^T, a lane then holds four consecutive columns of a row per register group;
 //  - tiles go to XCDs in contiguous ranges, row tiles fastest, so that a band of B stays in one L2.
-// A step takes the matrix core 32 cycles, at the rate of 4.9e15 operations per second that is four times a
-// large bf16 product's. Measured: 4096^3 39 us (3.5e15); 2048 x 1280, K = 5120, fp32 residual and output 15.7 us;
-// GEGLU 2048 x 5120, K = 1280 22.4 us; 32768 x 5120, K = 640 116.5 us (336 MB of output, 2.9 TB/s). The main
-// loop keeps the matrix cores 75 to 88 % busy; a tile's start (3.5 to 8 thousand cycles) and its stores and GELUs
-// (4 to 8) are what bounds the rest.
+// A step (65536 multiply-adds) takes the matrix core 32 cycles, 1.0e16 operations per second at 2.4 GHz, eight
+// times what a large bf16 product through the library reaches; a loop of steps on random data sustains 6.5 to
+// 7.1e15. Measured: 4096^3 40.9 us (3.4e15); 2048 x 1280, K = 5120, fp32 residual 15.5 us with a bf16 output, 19.4
+// with an fp32 one; GEGLU 2048 x 5120, K = 1280 23.1 us; 32768 x 5120, K = 640 116 us (336 MB of output, 2.9 TB/s).
+// The matrix cores are busy 51 % of the time that CUs are in the first, 20 to 30 % in the others: what bounds those
+// is a tile's start, which waits for residual, bias and first stages one after the other, and its stores and GELUs.
 #include <algorithm>
 #include <limits>
 #include <type_traits>
@@ -175,8 +176,9 @@ __device__ __forceinline__ void mx4_tile(const GemmMx4Params& p, const int m0, c
   const int nb0 = (n0 + wave * 32 * FN) / 32, nb_last = p.N / 32 - 1;
   const int bshift = FN == 1 ? 16 * (min(nb0, nb_last) & 1) : 0;
 
-  // The accumulators begin with residual and bias: their loads' latency lies beside the first stages' then,
-  // and the epilogue only stores. Lane: row r32 of block i, columns 8 g + 4 h .. + 3 in registers 4 g ...
+  // The accumulators begin with residual and bias, and the epilogue only stores. Both are waited for before the
+  // first stages' loads are issued: a latency each at a tile's start. Lane: row r32 of block i, columns
+  // 8 g + 4 h .. + 3 in registers 4 g ...
   // Rows are accessed in the store layout of a block, 64 bytes of each of 16 rows: row r16 and, for fp32 (a
   // pair of groups) and for bf16, the lane's first column.
   f32x16 acc[FM][FN];

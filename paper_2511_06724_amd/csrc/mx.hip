@@ -4,8 +4,9 @@
 // Both directions move bytes and do little else. A thread handles eight values (16 or 32 bytes of
 // the source, 4 or 8 of codes), four neighbouring lanes a block, whose largest magnitude meets in
 // two DPP steps. Slots are looked up once per row and workgroup. Bound by memory where rows are many: 100000 rows of
-// 768 fp16 values into scattered slots of a table of E2M1 rows 47 us and 10 for the claims (195 MB: 38 us at
-// 5.1 TB/s; in order 36), back as fp32 87 us (348 MB, 68); with one group of eight per thread instead of two 55 and 91.
+// 768 fp16 values into scattered slots of a table of E2M1 rows 59 us and 10 for the claims (195 MB: 38 us at
+// 5.1 TB/s; in order 39), back as fp32 75 us (348 MB, 68); two groups of eight per thread take the store 15 % and the
+// read 4 % less than one.
 #include <algorithm>
 
 #include "mx.h"
@@ -19,7 +20,9 @@ constexpr int kFetchGroups = 256 * kFetchUnroll;
 // Rows per call up to which every workgroup looks for later rows of its rows' slots by itself; more are
 // claimed by kernels of their own (64 states of 65536 values: 9.5 us with those).
 constexpr int kScanRows = 256;
-constexpr int kClaimOneGroup = 16384;   // rows one workgroup claims in a single launch
+// Rows one workgroup claims in a single launch, in dependent rounds: 17.5 us for 4096 rows, 51 for 16384. (The two
+// launches over a grid take 10 us for 100000.)
+constexpr int kClaimOneGroup = 16384;
 
 // Elements [c, c + 8) of a row, zero past `cols`; a row may begin at any element.
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Eight {

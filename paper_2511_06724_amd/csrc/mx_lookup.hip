@@ -7,11 +7,13 @@
 //
 // Rows of 8 .. 1024 values (mx_scan_mfma_kernel): codes converted to fp16 (exact) against up to 64 queries (32 past
 // 768 values) held in registers, on the matrix cores; the table is read once per pass, 17/32 (33/32) bytes a value.
-// Bound by that for few queries: 100000 x 768 E2M1 rows (41 MB) 13.1 us with the reduction for one query (one
-// pass at 5.1 TB/s: 8.0), 13.9 for 16; a million rows 73.4 (79.7). For 64 queries 21.8: a third of it the
-// queries' way into the registers of every CU (98 KB each), the rest products and conversions (16 cycles per
-// product, 8 per conversion of two values).
-// Other rows (mx_scan_kernel): two queries per pass (one past 8192 values), packed dot products in fp32.
+// Bound by that for few queries: 100000 x 768 E2M1 rows (41 MB) 10.8 us for one query (one pass at 5.1 TB/s: 8.0),
+// 11.1 for 16, a million rows 66.0 (79.7; from the cache between memory and L2 in part), E4M3 rows (79 MB) 16.9
+// (15.5), and 4 to 5 for the reduction. For 64 queries 19.0 (E4M3 24.1): a third of it the queries' way into the
+// registers of every CU (98 KB each), the rest products and conversions (16 cycles per product, 8 per conversion of
+// two values).
+// Other rows (mx_scan_kernel): two queries per pass (one past 8192 values), packed dot products in fp32; 100000 x
+// 1280 E2M1 rows (68 MB) 24 to 26 us a pass.
 #include <algorithm>
 #include <type_traits>
 
