@@ -280,3 +280,71 @@ def test_sdxl_step_properties_with_a_4_bit_feed_forward():
     assert e8 < e4
     del blob
     torch.cuda.empty_cache()
+
+
+# ----------------------------------------------------------------------------- at once, and at the limits
+
+@pytest.mark.parametrize("n,dim", [(200, 33), (4000, 96)])
+def test_calls_at_once(n, dim):
+    """Two streams store into alternate slots of one table (neighbours' scales share words and lines), then search
+    and read it, each with workspaces of its own: as one after the other."""
+    announce(f"mx stores, searches and fetches on two streams, {n} x {dim}")
+    fmt = dn.DN_MXFP8
+    x = f32_dev(_rng(n, dim, 41).standard_normal((n, dim))).half()
+    want = dn.mx_quantize(fmt, x)[:n * 33 * (-(-dim // 32))]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for rep in range(5):
+        table = _u8(dn.mx_bytes(fmt, n, dim), rep)
+        slots = [torch.arange(i, n, 2, device=DEV) for i in range(2)]
+        rows = [x[i::2].contiguous() for i in range(2)]
+        ws = [_u8(max(1, dn.ac_mx_store_bytes(len(s), n))) for s in slots]
+        lws = [_u8(dn.ac_mx_lookup_bytes(40, n, dim)) for _ in range(2)]
+        idx = [torch.full((40,), -5, device=DEV) for _ in range(2)]
+        out = [torch.zeros(40, dim, device=DEV) for _ in range(2)]
+        q = [x[i:i + 80:2].contiguous() for i in range(2)]
+        torch.cuda.synchronize()
+        for i, st in enumerate(streams):
+            dn.ac_mx_store(fmt, rows[i], slots[i], table, n, ws[i], stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(table[:want.numel()], want), rep
+        for i, st in enumerate(streams):
+            dn.ac_mx_lookup(fmt, q[i], table, n, lws[i], idx[i], stream=st)
+            dn.ac_mx_fetch(fmt, table, n, idx[i], out[i], stream=st)
+        torch.cuda.synchronize()
+        values = dn.mx_dequantize(fmt, table, n, dim)
+        for i in range(2):
+            assert idx[i].tolist() == list(range(i, i + 80, 2)) and torch.equal(out[i], values[idx[i]]), rep
+
+
+def test_the_longest_row():
+    """2^31 - 32 values in a row are the blocks of as many rows of 32 values: the same bytes, and the same values."""
+    cols, rows = 2 ** 31 - 32, 2 ** 26 - 1
+    announce(f"mx row of {cols} values")
+    x = torch.empty(cols, device=DEV, dtype=torch.bfloat16).normal_(generator=torch.Generator(device=DEV).manual_seed(3))
+    for fmt in (dn.DN_MXFP4, dn.DN_MXFP8):
+        a, b = dn.mx_quantize(fmt, x.view(1, cols)), dn.mx_quantize(fmt, x.view(rows, 32))
+        used = rows * (17 if fmt == dn.DN_MXFP4 else 33)
+        assert torch.equal(a[:used], b[:used])
+        del b
+        y = dn.mx_dequantize(fmt, a, 1, cols)
+        for at in (0, 2 ** 30, cols - 2 ** 20):
+            part = dn.mx_dequantize(fmt, dn.mx_quantize(fmt, x[at:at + 2 ** 20].view(-1, 32)), 2 ** 15, 32)
+            assert torch.equal(y[0, at:at + 2 ** 20], part.view(-1)), at
+        del a, y
+    del x
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M,N,K", [(33, 2 ** 22, 128), (3, 32, 2 ** 22)])
+def test_the_widest_and_the_deepest_product(M, N, K):
+    """Values of -1, 0 and 1, which the format holds: the sums are whole numbers below 2^24, exact in any order."""
+    announce(f"mx4 linear {M}x{N}x{K}")
+    g = torch.Generator(device=DEV).manual_seed(5)
+    x, w = (torch.randint(-1, 2, (r, K), device=DEV, generator=g).float() for r in (M, N))
+    y = torch.empty(M, N, device=DEV)
+    dn.op_linear(F4, dn.mx_quantize(F4, x), dn.pack_weight(F4, w, N, K), None, y, M, N, K, y_f32=True)
+    step = min(N, 2 ** 18)
+    for at in range(0, N, step):
+        assert torch.equal(y[:, at:at + step].double(), x.double() @ w[at:at + step].double().t().contiguous()), at
+    del x, w, y
+    torch.cuda.empty_cache()
