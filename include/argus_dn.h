@@ -22,6 +22,9 @@
  *   dn_mx_*                            microscaled (4- and 8-bit) rows: sizes, quantisation and back
  *   ac_mx_store / ac_mx_fetch          quantise cached states or embeddings as they are written, read them back
  *   ac_mx_lookup                       the nearest-prompt search over embeddings held in microscaled rows
+ *   dn_rope_table, dn_op_rope          rotary positions with one to four axes
+ *   dn_op_qk_norm_rope                 norms of query and key heads and the rotation, written to a cache
+ *   dn_op_attention_packed             grouped-head attention of packed sequences over that cache
  *   dn_unet_eps                        one UNet evaluation + guidance (per-step check hook)
  *   dn_vae_*                           the latent decoder after the loop (Table 3's VAE Decoder)
  *   dn_op_*                            single-kernel entry points (kernel checks, timing)
@@ -364,6 +367,98 @@ dn_status ac_mx_lookup_bytes(int32_t nq, int64_t n, int32_t dim, int64_t* bytes)
 dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, const void* table, int64_t n,
                        int32_t dim, const ac_k_table* levels, int64_t* out_idx, float* out_score, int32_t* out_k,
                        void* ws, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Packed sequences: the attention layer of transformers whose positions enter by rotation, between
+ * the input projection and the output projection. Rows of several requests of different lengths lie back
+ * to back (prompts, images' tokens, the next token of each of many requests); their keys and
+ * values may live in a cache that grows from call to call. All calls are asynchronous on `stream`,
+ * allocate nothing and keep no state, so calls on different buffers may overlap and be captured.
+ *
+ * Tensors of heads are device memory in the element type `dtype` (DN_BF16 or DN_FP32), rows `ld`
+ * elements apart, head h in columns [h * head_dim, (h + 1) * head_dim): a slice of a wider projection
+ * output is such a tensor. Rows are 16-byte aligned (pointer and ld); other buffers are aligned to their
+ * elements. Inputs and outputs do not overlap, unless said.
+ * ------------------------------------------------------------------------- */
+
+/* The sequences of a call; the arrays are device memory, read when the work runs, so a captured
+ * call follows their contents.
+ * Sequence s has the packed rows [q_start[s], q_start[s + 1]) and the key and value rows
+ * [kv_start[s], kv_start[s] + kv_len[s]); its last packed row belongs to its last key. A sequence may be
+ * empty. Sequences whose rows lie outside the call's tensors (or, in dn_op_qk_norm_rope, have fewer keys than
+ * packed rows) are skipped: their outputs are left as they were, and so are packed rows that
+ * belong to no sequence.
+ * max_kv_len: a bound of kv_len the caller knows; it decides how far the keys are split over the GPU and the
+ * size of the workspace, never the result's validity. */
+typedef struct {
+  int32_t n;
+  int32_t max_kv_len;
+  const int32_t* q_start;  /* [n + 1], non-decreasing */
+  const int64_t* kv_start; /* [n] */
+  const int32_t* kv_len;   /* [n] */
+} dn_sequences;
+
+/* Rotary positions (Su et al. 2021): pair i of a head, (a, b), becomes
+ *   (a cos t - b sin t, a sin t + b cos t),  t = pos[row][axis_i] * freqs[i],
+ * for the rot_dim / 2 pairs of the first rot_dim values; the other values pass unchanged. Pairs are
+ * neighbours (DN_ROPE_PAIRS: values 2i, 2i + 1) or half the rotated width apart (DN_ROPE_HALVES: values i,
+ * i + rot_dim / 2; rot_dim % 8 == 0). With several axes (time, height, width) the first axis_dims[0] / 2 pairs
+ * turn with axis 0, the next axis_dims[1] / 2 with axis 1, and so on. Positions are any int32; the angle
+ * is exact to 2^-31 of a turn at any of them. Negated positions turn back: the inverse,
+ * and the gradient. */
+#define DN_ROPE_MAX_AXES 4
+#define DN_ROPE_MAX_DIM 256
+#define DN_ROPE_TABLE_BYTES 2048
+typedef enum { DN_ROPE_PAIRS = 0, DN_ROPE_HALVES = 1 } dn_rope_pairing;
+
+/* Fills `table` (device, DN_ROPE_TABLE_BYTES, 16-byte aligned) for sum(axis_dims) / 2 pairs: freqs host double,
+ * radians per position (finite, magnitude at most 65536); axis_dims host int32 [n_axes], even, at most
+ * DN_ROPE_MAX_DIM together. Both are read during the call. A table serves any number of calls. */
+dn_status dn_rope_table(const double* freqs, const int32_t* axis_dims, int32_t n_axes, void* table, void* stream);
+
+typedef struct {
+  const void* table;  /* device, of dn_rope_table with the same axes and rot_dim = sum(axis_dims) */
+  const int32_t* pos; /* device [T][n_axes] */
+  int32_t n_axes;
+  int32_t rot_dim;
+  int32_t pairing;
+} dn_rotation;
+
+/* y = the rotated heads of x [T][ldx]; y [T][ldy] may be x (with one stride). head_dim a multiple of 8, at most
+ * DN_ROPE_MAX_DIM; 1 <= T < 2^31. fp32 inside, one rounding. */
+dn_status dn_op_rope(int32_t dtype, const void* x, int64_t ldx, void* y, int64_t ldy, int64_t T, int32_t heads,
+                     int32_t head_dim, const dn_rotation* rot, void* stream);
+
+/* RMS norm of every query and key head, then the rotation, in one pass:
+ *   y = rotate(x / sqrt(mean(x^2) + eps) * gain)   (mean over the head_dim values; fp32 inside, one rounding)
+ * for the `heads` heads of q [T][ldq] with q_gain and the `kv_heads` heads of k [T][ldk] with k_gain (fp32
+ * [head_dim]), to q_out [T][ldqo] and k_out. v [T][ldv] (or NULL, with v_out NULL) is copied to v_out.
+ * seqs NULL: row t of k (v) goes to row t of k_out (v_out); outputs may be their inputs.
+ * With seqs: k_out and v_out are a cache of kv_rows rows, and packed row i of the n_s rows of sequence s
+ *   goes to cache row kv_start[s] + kv_len[s] - n_s + i (kv_len counts the new rows). Sequences must not share
+ *   the rows they write. */
+dn_status dn_op_qk_norm_rope(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                             int64_t ldv, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                             const float* q_gain, const float* k_gain, float eps, const dn_rotation* rot,
+                             const dn_sequences* seqs, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* v_out,
+                             int64_t ldvo, int64_t kv_rows, void* stream);
+
+/* o = softmax(q k^T * scale) v for every sequence and query head h, over the keys and values of key head
+ * h / (heads / kv_heads): q [T][ldq], o [T][ldo], k [kv_rows][ldk], v [kv_rows][ldv], head_dim 32, 64, 96 or
+ * 128, heads a multiple of kv_heads. causal = 1: packed row i of the n_s of a sequence sees its first
+ * kv_len - n_s + i + 1 keys; 0: all. A row that sees no key (or whose keys all score -inf) gives
+ * zeros. Keys a row does not see have no influence on it, whatever they hold. Softmax and sums
+ * fp32; bf16 probabilities enter the product rounded to bf16.
+ * T * (heads / kv_heads) < 2^31 - 65536.
+ * ws: device, 16-byte aligned, dn_attention_packed_bytes bytes (0: NULL) for the same T, heads, n and
+ * max_kv_len, contents arbitrary, free when the call's work has finished; overlapping calls need workspaces of
+ * their own. */
+dn_status dn_attention_packed_bytes(int32_t dtype, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t n,
+                                    int32_t max_kv_len, int64_t* bytes);
+dn_status dn_op_attention_packed(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                                 int64_t ldv, void* o, int64_t ldo, int64_t T, int64_t kv_rows, int32_t heads,
+                                 int32_t kv_heads, int32_t head_dim, const dn_sequences* seqs, int32_t causal, float scale,
+                                 void* ws, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Single-kernel entry points. They run exactly the kernels dn_denoise runs and

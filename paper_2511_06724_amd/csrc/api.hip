@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "model.h"
+#include "packed.h"
 
 // Scratch of the no-allocation batched lookup: the per-workgroup winners of one pass
 // (at most lookup_batch_workspace_bytes(), 256 KiB, which also covers the per-query
@@ -302,6 +303,67 @@ template <typename T> void op_gemm(dn::GemmParams& p, hipStream_t s) {
     dn::gemm_fp8(p, g, s);
   else
     dn::gemm<T>(p, g, s);
+}
+
+// ---------------------------------------------------------------- packed sequences
+
+// Rows of a tensor of heads: 16-byte aligned, at least `width` and a multiple of 16 bytes apart.
+void check_heads(const char* who, int32_t dtype, const void* x, int64_t ld, int64_t width) {
+  const int64_t vec = dtype == DN_BF16 ? 8 : 4;
+  DN_CHECK(x, std::string(who) + ": null pointer");
+  DN_CHECK(on(x, 16), std::string(who) + ": rows must be 16-byte aligned");
+  DN_CHECK(ld >= width && ld % vec == 0 && ld <= (1ll << 40),
+           std::string(who) + ": row stride must cover the heads and be a multiple of 16 bytes");
+}
+
+dn::Sequences sequences(const char* who, const dn_sequences* s) {
+  DN_CHECK(s->n >= 1, std::string(who) + ": at least one sequence");
+  DN_CHECK(s->q_start && s->kv_start && s->kv_len, std::string(who) + ": null pointer in the sequences");
+  DN_CHECK(on(s->q_start, 4) && on(s->kv_start, 8) && on(s->kv_len, 4), std::string(who) + ": misaligned sequences");
+  DN_CHECK(s->max_kv_len >= 1, std::string(who) + ": max_kv_len must be positive");
+  dn::Sequences r;
+  r.n = s->n;
+  r.q_start = s->q_start;
+  r.kv_start = reinterpret_cast<const long long*>(s->kv_start);
+  r.kv_len = s->kv_len;
+  return r;
+}
+
+dn::RotaryParams rotation(const char* who, int32_t dtype, int64_t T, int32_t head_dim, const dn_rotation* r) {
+  DN_CHECK(is_dtype(dtype), std::string(who) + ": bad dtype");
+  DN_CHECK(T >= 1 && T <= 0x7fffffff, std::string(who) + ": bad row count");
+  DN_CHECK(head_dim >= 8 && head_dim <= DN_ROPE_MAX_DIM && head_dim % 8 == 0,
+           std::string(who) + ": head_dim must be a multiple of 8, at most 256");
+  DN_CHECK(r && r->table && r->pos, std::string(who) + ": null rotation, table or positions");
+  DN_CHECK(on(r->table, 16) && on(r->pos, 4), std::string(who) + ": misaligned table or positions");
+  DN_CHECK(r->n_axes >= 1 && r->n_axes <= DN_ROPE_MAX_AXES, std::string(who) + ": one to four axes");
+  DN_CHECK(r->pairing == DN_ROPE_PAIRS || r->pairing == DN_ROPE_HALVES, std::string(who) + ": bad pairing");
+  DN_CHECK(r->rot_dim >= 2 && r->rot_dim <= head_dim && r->rot_dim % 2 == 0,
+           std::string(who) + ": rot_dim must be even, 2 .. head_dim");
+  DN_CHECK(r->pairing == DN_ROPE_PAIRS || r->rot_dim % 8 == 0, std::string(who) + ": DN_ROPE_HALVES needs rot_dim % 8 == 0");
+  dn::RotaryParams p;
+  p.T = T;
+  p.D = head_dim;
+  p.table = static_cast<const dn::RopeEntry*>(r->table);
+  p.pos = r->pos;
+  p.n_axes = r->n_axes;
+  p.half = r->rot_dim / 2;
+  p.halves = r->pairing == DN_ROPE_HALVES;
+  return p;
+}
+
+void run_rotary(int32_t dtype, const dn::RotaryParams& p, void* stream) {
+  dtype == DN_BF16 ? dn::rotary<dn::bf16>(p, as_stream(stream)) : dn::rotary<float>(p, as_stream(stream));
+}
+
+void check_packed_sizes(const char* who, int32_t dtype, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim) {
+  DN_CHECK(is_dtype(dtype), std::string(who) + ": bad dtype");
+  DN_CHECK(T >= 1 && T <= 0x7fffffff, std::string(who) + ": bad row count");
+  DN_CHECK(heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0, std::string(who) + ": heads must be a multiple of kv_heads");
+  DN_CHECK(heads <= 65535, std::string(who) + ": at most 65535 heads");
+  DN_CHECK(dn::attention_packed_dim(head_dim), std::string(who) + ": head_dim must be 32, 64, 96 or 128");
+  // a sequence's rows (tokens times the heads of a group) are counted in 32 bits
+  DN_CHECK(T * (heads / kv_heads) <= 0x7fffffff - 65536, std::string(who) + ": too many rows");
 }
 
 }  // namespace
@@ -737,6 +799,136 @@ dn_status dn_op_attention(int32_t dtype, const void* q, int32_t ldq, const void*
       dn::attention<dn::bf16>(a, head_stride, cus, as_stream(stream));
     else
       dn::attention<float>(a, head_stride, cus, as_stream(stream));
+  });
+}
+
+dn_status dn_rope_table(const double* freqs, const int32_t* axis_dims, int32_t n_axes, void* table, void* stream) {
+  return guarded([&] {
+    DN_CHECK(freqs && axis_dims && table, "dn_rope_table: null pointer");
+    DN_CHECK(on(table, 16), "dn_rope_table: the table must be 16-byte aligned");
+    DN_CHECK(n_axes >= 1 && n_axes <= DN_ROPE_MAX_AXES, "dn_rope_table: one to four axes");
+    dn::RopeTableParams p = {};
+    int n = 0;
+    for (int a = 0; a < n_axes; ++a) {
+      DN_CHECK(axis_dims[a] >= 2 && axis_dims[a] % 2 == 0 && axis_dims[a] <= DN_ROPE_MAX_DIM - 2 * n,
+               "dn_rope_table: axis dims must be even and at most 256 together");
+      for (int j = 0; j < axis_dims[a] / 2; ++j, ++n) {
+        DN_CHECK(std::isfinite(freqs[n]) && std::fabs(freqs[n]) <= 65536.0,
+                 "dn_rope_table: frequencies must be finite, at most 65536");
+        long double turn = static_cast<long double>(freqs[n]) / 6.283185307179586476925286766559L;
+        turn -= std::floor(turn);
+        const long double f = std::round(std::ldexp(turn, 64));
+        p.turn[n] = f >= 18446744073709551616.0L ? 0 : static_cast<unsigned long long>(f);
+        p.axis[n] = static_cast<unsigned char>(a);
+      }
+    }
+    dn::rope_table(p, table, as_stream(stream));
+  });
+}
+
+dn_status dn_op_rope(int32_t dtype, const void* x, int64_t ldx, void* y, int64_t ldy, int64_t T, int32_t heads,
+                     int32_t head_dim, const dn_rotation* rot, void* stream) {
+  return guarded([&] {
+    dn::RotaryParams p = rotation("dn_op_rope", dtype, T, head_dim, rot);
+    DN_CHECK(heads >= 1 && heads <= 65535, "dn_op_rope: bad head count");
+    check_heads("dn_op_rope", dtype, x, ldx, (int64_t)heads * head_dim);
+    check_heads("dn_op_rope", dtype, y, ldy, (int64_t)heads * head_dim);
+    DN_CHECK(x != y || ldx == ldy, "dn_op_rope: in place needs one row stride");
+    p.q = x;
+    p.qo = y;
+    p.ldq = ldx;
+    p.ldqo = ldy;
+    p.heads = heads;
+    run_rotary(dtype, p, stream);
+  });
+}
+
+dn_status dn_op_qk_norm_rope(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                             int64_t ldv, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                             const float* q_gain, const float* k_gain, float eps, const dn_rotation* rot,
+                             const dn_sequences* seqs, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* v_out,
+                             int64_t ldvo, int64_t kv_rows, void* stream) {
+  return guarded([&] {
+    const char* who = "dn_op_qk_norm_rope";
+    dn::RotaryParams p = rotation(who, dtype, T, head_dim, rot);
+    DN_CHECK(heads >= 1 && heads <= 65535 && kv_heads >= 1 && kv_heads <= 65535, "dn_op_qk_norm_rope: bad head counts");
+    DN_CHECK(q_gain && k_gain && on(q_gain, 4) && on(k_gain, 4), "dn_op_qk_norm_rope: null or misaligned gains");
+    DN_CHECK(eps >= 0.f && std::isfinite(eps), "dn_op_qk_norm_rope: eps must be finite and not negative");
+    DN_CHECK((v == nullptr) == (v_out == nullptr), "dn_op_qk_norm_rope: values and their output go together");
+    const int64_t wq = (int64_t)heads * head_dim, wk = (int64_t)kv_heads * head_dim;
+    check_heads(who, dtype, q, ldq, wq);
+    check_heads(who, dtype, q_out, ldqo, wq);
+    check_heads(who, dtype, k, ldk, wk);
+    check_heads(who, dtype, k_out, ldko, wk);
+    if (v) {
+      check_heads(who, dtype, v, ldv, wk);
+      check_heads(who, dtype, v_out, ldvo, wk);
+    }
+    DN_CHECK(q != q_out || ldq == ldqo, "dn_op_qk_norm_rope: in place needs one row stride");
+    if (seqs) {
+      DN_CHECK(k != k_out && (!v || v != v_out), "dn_op_qk_norm_rope: with sequences keys and values are not written in place");
+      DN_CHECK(kv_rows >= 1 && kv_rows <= (1ll << 40), "dn_op_qk_norm_rope: bad kv_rows");
+      p.seqs = sequences(who, seqs);
+      p.kv_rows = kv_rows;
+    } else {
+      DN_CHECK((k != k_out || ldk == ldko) && (!v || v != v_out || ldv == ldvo), "dn_op_qk_norm_rope: in place needs one row stride");
+    }
+    p.q = q, p.k = k, p.v = v, p.qo = q_out, p.ko = k_out, p.vo = v_out;
+    p.ldq = ldq, p.ldk = ldk, p.ldv = ldv, p.ldqo = ldqo, p.ldko = ldko, p.ldvo = ldvo;
+    p.heads = heads;
+    p.kv_heads = kv_heads;
+    p.v_heads = v ? kv_heads : 0;
+    p.gq = q_gain;
+    p.gk = k_gain;
+    p.eps = eps;
+    run_rotary(dtype, p, stream);
+  });
+}
+
+dn_status dn_attention_packed_bytes(int32_t dtype, int64_t T, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t n,
+                                    int32_t max_kv_len, int64_t* bytes) {
+  return guarded([&] {
+    DN_CHECK(bytes, "dn_attention_packed_bytes: null pointer");
+    check_packed_sizes("dn_attention_packed_bytes", dtype, T, heads, kv_heads, head_dim);
+    DN_CHECK(n >= 1 && max_kv_len >= 1, "dn_attention_packed_bytes: bad sizes");
+    *bytes = static_cast<int64_t>(
+        dn::attention_packed_bytes(dtype == DN_BF16 ? 2 : 4, T, heads, kv_heads, head_dim, n, max_kv_len));
+  });
+}
+
+dn_status dn_op_attention_packed(int32_t dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                                 int64_t ldv, void* o, int64_t ldo, int64_t T, int64_t kv_rows, int32_t heads,
+                                 int32_t kv_heads, int32_t head_dim, const dn_sequences* seqs, int32_t causal, float scale,
+                                 void* ws, void* stream) {
+  return guarded([&] {
+    const char* who = "dn_op_attention_packed";
+    check_packed_sizes(who, dtype, T, heads, kv_heads, head_dim);
+    DN_CHECK(kv_rows >= 1 && kv_rows <= (1ll << 40), "dn_op_attention_packed: bad kv_rows");
+    DN_CHECK(seqs, "dn_op_attention_packed: null sequences");
+    DN_CHECK(causal == 0 || causal == 1, "dn_op_attention_packed: causal is 0 or 1");
+    DN_CHECK(std::isfinite(scale), "dn_op_attention_packed: the scale must be finite");
+    const int64_t wq = (int64_t)heads * head_dim, wk = (int64_t)kv_heads * head_dim;
+    check_heads(who, dtype, q, ldq, wq);
+    check_heads(who, dtype, k, ldk, wk);
+    check_heads(who, dtype, v, ldv, wk);
+    check_heads(who, dtype, o, ldo, wq);
+    dn::PackedAttnParams p;
+    p.seqs = sequences(who, seqs);
+    p.q = q, p.k = k, p.v = v, p.o = o;
+    p.ldq = ldq, p.ldk = ldk, p.ldv = ldv, p.ldo = ldo;
+    p.T = T;
+    p.kv_rows = kv_rows;
+    p.heads = heads;
+    p.kv_heads = kv_heads;
+    p.max_kv = seqs->max_kv_len;
+    p.causal = causal != 0;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.ws = ws;
+    DN_CHECK(ws ? on(ws, 16)
+                : dn::attention_packed_bytes(dtype == DN_BF16 ? 2 : 4, T, heads, kv_heads, head_dim, seqs->n, p.max_kv) == 0,
+             "dn_op_attention_packed: the workspace of dn_attention_packed_bytes is needed, 16-byte aligned");
+    dtype == DN_BF16 ? dn::attention_packed<dn::bf16>(p, head_dim, as_stream(stream))
+                     : dn::attention_packed<float>(p, head_dim, as_stream(stream));
   });
 }
 

@@ -19,6 +19,8 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libargus_d
 DN_OK, DN_EINVAL, DN_ENOMEM, DN_EHIP, DN_EUNSUPPORTED = 0, -1, -2, -3, -4
 DN_FP32, DN_BF16, DN_FP8, DN_MXFP4, DN_MXFP8, DN_FP16 = 0, 1, 2, 3, 4, 5
 DN_WEIGHTS_HOST, DN_WEIGHTS_DEVICE = 0, 1
+DN_ROPE_PAIRS, DN_ROPE_HALVES = 0, 1
+DN_ROPE_TABLE_BYTES = 2048
 ABI_VERSION = 1
 MAX_LEVELS = 4
 
@@ -28,7 +30,8 @@ EXPORTED = ("dn_weight_count", "dn_weight_table", "dn_create", "dn_denoise", "dn
             "dn_probe_mfma_rate",
             "dn_destroy", "dn_last_error", "dn_vae_weight_count", "dn_vae_weight_table", "dn_vae_create",
             "dn_vae_decode", "dn_vae_destroy", "dn_mx_bytes", "dn_mx_quantize", "dn_mx_dequantize", "ac_mx_store_bytes",
-            "ac_mx_store", "ac_mx_fetch", "ac_mx_lookup_bytes", "ac_mx_lookup", "argus_oda", "argus_route", "argus_select_worker", "argus_last_error")
+            "ac_mx_store", "ac_mx_fetch", "ac_mx_lookup_bytes", "ac_mx_lookup", "dn_rope_table", "dn_op_rope", "dn_op_qk_norm_rope",
+            "dn_attention_packed_bytes", "dn_op_attention_packed", "argus_oda", "argus_route", "argus_select_worker", "argus_last_error")
 
 
 AC_MAX_K_LEVELS = 16
@@ -71,6 +74,16 @@ class _VaeConfig(C.Structure):
     ]
 
 
+class _Sequences(C.Structure):
+    _fields_ = [("n", C.c_int32), ("max_kv_len", C.c_int32), ("q_start", C.c_void_p), ("kv_start", C.c_void_p),
+                ("kv_len", C.c_void_p)]
+
+
+class _Rotation(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("pos", C.c_void_p), ("n_axes", C.c_int32), ("rot_dim", C.c_int32),
+                ("pairing", C.c_int32)]
+
+
 def _load():
     # One HIP runtime per process: PyTorch bundles its own libamdhip64 with the
     # same soname as ROCm's. Importing torch first makes the library bind to that
@@ -101,6 +114,13 @@ def _load():
         "ac_mx_fetch": [I32, P, I64, I64, P, I64, P, I64, P],
         "ac_mx_lookup_bytes": [I32, I64, I32, C.POINTER(I64)],
         "ac_mx_lookup": [I32, P, I32, P, I64, I32, C.POINTER(_KTable), P, P, P, P, P],
+        "dn_rope_table": [P, P, I32, P, P],
+        "dn_op_rope": [I32, P, I64, P, I64, I64, I32, I32, C.POINTER(_Rotation), P],
+        "dn_op_qk_norm_rope": [I32, P, I64, P, I64, P, I64, I64, I32, I32, I32, P, P, F32, C.POINTER(_Rotation),
+                               C.POINTER(_Sequences), P, I64, P, I64, P, I64, I64, P],
+        "dn_attention_packed_bytes": [I32, I64, I32, I32, I32, I32, I32, C.POINTER(I64)],
+        "dn_op_attention_packed": [I32, P, I64, P, I64, P, I64, P, I64, I64, I64, I32, I32, I32, C.POINTER(_Sequences), I32,
+                                   F32, P, P],
         "dn_packed_weight_elems": [I32, I32, I32, C.POINTER(I64)],
         "dn_pack_weight": [I32, P, I32, I32, P, P],
         "dn_op_linear": [I32, P, P, P, P, I32, P, I32, I64, I32, I32, I32, P],
@@ -526,6 +546,160 @@ def ac_mx_lookup(dtype, queries, table, n, ws, out_idx, out_score=None, out_k=No
         tab = C.byref(k_table(thresholds, levels))
     _check(lib.ac_mx_lookup(dtype, _ptr(queries), nq, _ptr(table), n, dim, tab, _ptr(out_idx), _ptr(out_score),
                             _ptr(out_k), _ptr(ws), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- packed sequences
+
+@functools.lru_cache(maxsize=None)
+def _head_types():
+    import torch
+    return {torch.float32: DN_FP32, torch.bfloat16: DN_BF16}
+
+
+def _heads(x, name):
+    """(dtype, row stride, rows, heads, head_dim) of a tensor of heads: [rows, heads, head_dim] with dense heads
+    side by side (a slice of a wider projection output is one)."""
+    if x.dim() != 3:
+        raise ValueError(f"{name}: a tensor [rows, heads, head_dim] is needed")
+    (rows, heads, dim), (ld, sh, sd) = x.shape, x.stride()
+    if (dim > 1 and sd != 1) or (heads > 1 and sh != dim):
+        raise ValueError(f"{name}: the heads of a row must be dense, side by side")
+    dt = _head_types().get(x.dtype)
+    if dt is None:
+        raise ValueError(f"{name}: heads must be float32 or bfloat16")
+    return dt, heads * dim if rows == 1 and ld < heads * dim else ld, rows, heads, dim
+
+
+def _dense(t, dtype, shape, name):
+    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: a dense {dtype} tensor {list(shape)} is needed")
+
+
+class Sequences:
+    """The sequences of a packed batch: q_start int32 [n + 1], kv_start int64 [n], kv_len int32 [n] (CUDA tensors, read
+    when the work runs), and a bound of kv_len the caller knows."""
+
+    def __init__(self, q_start, kv_start, kv_len, max_kv_len):
+        import torch
+        n = kv_len.shape[0] if kv_len.dim() == 1 else -1
+        _dense(kv_len, torch.int32, (n,), "Sequences: kv_len")
+        _dense(kv_start, torch.int64, (n,), "Sequences: kv_start")
+        _dense(q_start, torch.int32, (n + 1,), "Sequences: q_start")
+        self.n, self.max_kv_len = n, int(max_kv_len)
+        self._keep = (q_start, kv_start, kv_len)
+        self._c = _Sequences(n, self.max_kv_len, _ptr(q_start), _ptr(kv_start), _ptr(kv_len))
+
+
+def rope_freqs(axis_dims, theta=10000.0, per_axis=True):
+    """Frequencies of every rotated pair in axis order: theta^(-2 i / d), over the dims d of its own axis (per_axis)
+    or of all axes together."""
+    total, out = sum(axis_dims), []
+    for d in axis_dims:
+        for j in range(d // 2):
+            out.append(float(theta) ** (-2.0 * j / d if per_axis else -2.0 * len(out) / total))
+    return out
+
+
+class RopeTable:
+    """A rotation table on the GPU (dn_rope_table)."""
+
+    def __init__(self, axis_dims, freqs, device, stream=None):
+        import torch
+        self.axis_dims = tuple(int(d) for d in axis_dims)
+        dims = np.ascontiguousarray(self.axis_dims, dtype=np.int32)
+        f = np.ascontiguousarray(freqs, dtype=np.float64)
+        if dims.ndim != 1 or f.shape != (sum(self.axis_dims) // 2,):
+            raise ValueError("rope_table: one frequency per rotated pair is needed")
+        self.rot_dim, self.n_axes = sum(self.axis_dims), len(self.axis_dims)
+        self.data = torch.empty(DN_ROPE_TABLE_BYTES, device=device, dtype=torch.uint8)
+        _check(lib.dn_rope_table(f.ctypes.data, dims.ctypes.data, self.n_axes, _ptr(self.data), _stream(stream)))
+
+
+def rope_table(axis_dims, theta=10000.0, per_axis=True, freqs=None, device="cuda", stream=None):
+    """The table of a rotation over axes of axis_dims rotated values each (time, height, width, ...); freqs: radians per
+    position of every pair (default rope_freqs)."""
+    return RopeTable(axis_dims, rope_freqs(axis_dims, theta, per_axis) if freqs is None else freqs, device, stream)
+
+
+def _rotation(table, pos, rows, pairing, name):
+    import torch
+    _dense(pos, torch.int32, (rows, table.n_axes), f"{name}: pos")
+    return C.byref(_Rotation(_ptr(table.data), _ptr(pos), table.n_axes, table.rot_dim, pairing))
+
+
+def op_rope(x, pos, table, y=None, pairing=DN_ROPE_PAIRS, stream=None):
+    """Rotates the heads of x [rows, heads, head_dim] to pos int32 [rows, axes] (into y, a new tensor, or x itself)."""
+    import torch
+    dt, ldx, rows, heads, dim = _heads(x, "op_rope")
+    if y is None:
+        y = torch.empty(rows, heads, dim, device=x.device, dtype=x.dtype)
+    yt, ldy, *shape = _heads(y, "op_rope: y")
+    if yt != dt or shape != [rows, heads, dim]:
+        raise ValueError("op_rope: y must have the type and shape of x")
+    _check(lib.dn_op_rope(dt, _ptr(x), ldx, _ptr(y), ldy, rows, heads, dim, _rotation(table, pos, rows, pairing, "op_rope"),
+                          _stream(stream)))
+    return y
+
+
+def op_qk_norm_rope(q, k, q_gain, k_gain, eps, pos, table, q_out, k_out, v=None, v_out=None, seqs=None,
+                    pairing=DN_ROPE_PAIRS, stream=None):
+    """RMS norm and rotation of every head of q and k [rows, heads, head_dim] into q_out and k_out, v copied to v_out;
+    with seqs (Sequences) k_out and v_out are caches whose rows the sequences own."""
+    import torch
+    name = "op_qk_norm_rope"
+    dt, ldq, rows, heads, dim = _heads(q, f"{name}: q")
+    kt, ldk, k_rows, kv_heads, k_dim = _heads(k, f"{name}: k")
+    qot, ldqo, *q_shape = _heads(q_out, f"{name}: q_out")
+    kot, ldko, out_rows, *ko_shape = _heads(k_out, f"{name}: k_out")
+    if (kt, qot, kot) != (dt, dt, dt) or (k_rows, k_dim) != (rows, dim) or q_shape != [rows, heads, dim]:
+        raise ValueError(f"{name}: types, rows and head widths of q, k and their outputs must agree")
+    if ko_shape != [kv_heads, dim] or (seqs is None and out_rows != rows):
+        raise ValueError(f"{name}: k_out must have the heads of k, and its rows where there are no sequences")
+    ldv = ldvo = 0
+    if (v is None) != (v_out is None):
+        raise ValueError(f"{name}: values and their output go together")
+    if v is not None:
+        vt, ldv, *v_shape = _heads(v, f"{name}: v")
+        vot, ldvo, *vo_shape = _heads(v_out, f"{name}: v_out")
+        if (vt, vot) != (dt, dt) or v_shape != [rows, kv_heads, dim] or vo_shape != [out_rows, kv_heads, dim]:
+            raise ValueError(f"{name}: values must have the type and shape of the keys, and so must their output")
+    _dense(q_gain, torch.float32, (dim,), f"{name}: q_gain")
+    _dense(k_gain, torch.float32, (dim,), f"{name}: k_gain")
+    _check(lib.dn_op_qk_norm_rope(dt, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, rows, heads, kv_heads, dim, _ptr(q_gain),
+                                  _ptr(k_gain), eps, _rotation(table, pos, rows, pairing, name),
+                                  C.byref(seqs._c) if seqs is not None else None, _ptr(q_out), ldqo, _ptr(k_out), ldko,
+                                  _ptr(v_out), ldvo, out_rows, _stream(stream)))
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_packed_bytes(dtype, rows, heads, kv_heads, dim, n, max_kv_len):
+    b = C.c_int64()
+    _check(lib.dn_attention_packed_bytes(dtype, rows, heads, kv_heads, dim, n, max_kv_len, C.byref(b)))
+    return b.value
+
+
+def attention_packed_bytes(q, k, seqs):
+    """Workspace bytes of op_attention_packed for tensors like q and k (0: none is needed)."""
+    dt, _, rows, heads, dim = _heads(q, "attention_packed_bytes: q")
+    return _attention_packed_bytes(dt, rows, heads, k.shape[1], dim, seqs.n, seqs.max_kv_len)
+
+
+def op_attention_packed(q, k, v, o, seqs, causal=True, scale=None, ws=None, stream=None):
+    """Attention of packed sequences: q, o [rows, heads, head_dim], k, v [kv_rows, kv_heads, head_dim]; scale: default
+    head_dim^-1/2; ws: uint8, attention_packed_bytes."""
+    name = "op_attention_packed"
+    dt, ldq, rows, heads, dim = _heads(q, f"{name}: q")
+    kt, ldk, *kv = _heads(k, f"{name}: k")
+    vt, ldv, *v_shape = _heads(v, f"{name}: v")
+    ot, ldo, *o_shape = _heads(o, f"{name}: o")
+    if (kt, vt, ot) != (dt, dt, dt) or o_shape != [rows, heads, dim] or kv != v_shape or kv[2] != dim:
+        raise ValueError(f"{name}: types and shapes of q, k, v and o must agree")
+    need = _attention_packed_bytes(dt, rows, heads, kv[1], dim, seqs.n, seqs.max_kv_len)
+    if ws is not None:
+        _buffer(ws, need, f"{name} workspace")
+    _check(lib.dn_op_attention_packed(dt, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(o), ldo, rows, kv[0], heads, kv[1], dim,
+                                      C.byref(seqs._c), int(causal), dim ** -0.5 if scale is None else scale,
+                                      _ptr(ws) if need else None, _stream(stream)))
 
 
 def packed_weight_elems(dtype, N, K):

@@ -1,0 +1,463 @@
+"""Rotary positions, norms of query and key heads with the rotation, and attention of packed sequences
+against the fp64 oracle.
+
+Tolerances. u is half a step of the output type relative to the value (fp32 2^-24, bf16 2^-8), w = 2^-24.
+Rotation: sine and cosine are within 4 w, a product and a sum round once more each: 8 w (|a| + |b|), then u |y|.
+Norm: a sum of squares of up to 256 values in groups of eight and a tree of five levels is within 13 w,
+its root half of that; root, quotient and two products round: 16 w in all, on both values of a pair.
+Attention: a score is a sum of dim products, within dim w sum|q k| scale; with the scaling and the difference
+to the reference maximum, four roundings of a score, that is the relative error d of a probability (and
+the exponential's own 2 w). bf16 probabilities round by u in the product. o = sum p v / sum p is then within
+2 (d + u_p) + (keys + 4) w of sum p |v|, then u |o|."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import packed as P
+from paper_2511_06724_amd import dn
+from tests.gpu_util import DEV, announce, host, tdtype
+
+pytestmark = pytest.mark.gpu
+
+W = 2.0 ** -24
+U = {dn.DN_FP32: 2.0 ** -24, dn.DN_BF16: 2.0 ** -8}
+TYPES = [dn.DN_FP32, dn.DN_BF16]
+
+
+def heads(rng, rows, n, dim, dtype, pad=0, std=1.0):
+    """A device tensor [rows, n, dim] (a slice of a wider one with `pad` heads behind) and its values."""
+    t = torch.from_numpy(rng.normal(size=(rows, n + pad, dim)).astype(np.float32) * std).to(DEV).to(tdtype(dtype))[:, :n]
+    return t, host(t)
+
+
+def int_t(a, dtype=torch.int32):
+    return torch.tensor(a, device=DEV, dtype=dtype)
+
+
+def positions(rng, rows, axes, far=False):
+    lo, hi = (-2 ** 31, 2 ** 31) if far else (-50, 5000)
+    p = rng.integers(lo, hi, (rows, axes)).astype(np.int32)
+    return torch.from_numpy(p).to(DEV), p
+
+
+def rope_tol(x, freqs, pairing, ref, dtype, w=8):
+    half = len(freqs)
+    a = np.abs(x)
+    first = slice(0, 2 * half, 2) if pairing == P.PAIRS else slice(0, half)
+    second = slice(1, 2 * half, 2) if pairing == P.PAIRS else slice(half, 2 * half)
+    s = a[..., first] + a[..., second]
+    t = w * W * a
+    t[..., first], t[..., second] = w * W * s, w * W * s
+    return t + U[dtype] * np.abs(ref)
+
+
+def close(got, ref, tol):
+    assert np.isfinite(got).all() and (np.abs(got - ref) <= tol).all(), float((np.abs(got - ref) - tol).max())
+
+
+ROPES = [(64, (32, 32), True), (128, (32, 48, 48), False), (80, (16, 24, 24), True), (128, (128,), True), (256, (256,), True),
+         (8, (8,), True), (16, (2, 2, 2, 2), False), (96, (16, 40), True), (32, (8,), True), (200, (160,), False)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pairing", [dn.DN_ROPE_PAIRS, dn.DN_ROPE_HALVES])
+@pytest.mark.parametrize("dim,axes,per_axis", ROPES)
+def test_rope(dtype, pairing, dim, axes, per_axis):
+    for rows, n, far in ((1, 1, True), (7, 5, False), (300, 13, True)):
+        announce(f"rope {dtype} {pairing} {dim} {axes} {rows} x {n}")
+        rng = np.random.default_rng(rows)
+        x, xv = heads(rng, rows, n, dim, dtype, pad=1)
+        pos, pv = positions(rng, rows, len(axes), far)
+        table = dn.rope_table(axes, 10000.0, per_axis)
+        freqs = dn.rope_freqs(axes, 10000.0, per_axis)
+        ref = P.rotate(xv, pv, freqs, axes, pairing)
+        y = dn.op_rope(x, pos, table, pairing=pairing)
+        close(host(y), ref, rope_tol(xv, freqs, pairing, ref, dtype))
+        # in place, on a strided tensor, and whatever lies behind it stays
+        whole = x._base if x._base is not None else x
+        behind = whole[:, n:].clone()
+        dn.op_rope(x, pos, table, x, pairing=pairing)
+        assert torch.equal(x, y) and torch.equal(whole[:, n:], behind)
+
+
+def test_rope_backwards_and_large_grid():
+    """Negated positions turn back; many rows take the variant of several heads a lane group."""
+    rng = np.random.default_rng(5)
+    x, xv = heads(rng, 9000, 9, 64, dn.DN_FP32)
+    pos, pv = positions(rng, 9000, 2)
+    table = dn.rope_table((32, 32))
+    y = dn.op_rope(x, pos, table)
+    ref = P.rotate(xv, pv, dn.rope_freqs((32, 32)), (32, 32), P.PAIRS)
+    close(host(y), ref, rope_tol(xv, dn.rope_freqs((32, 32)), P.PAIRS, ref, dn.DN_FP32))
+    back = dn.op_rope(y, -pos, table)
+    assert (back - x).abs().max().item() <= 2 * 16 * W * 2 * x.abs().max().item()
+    few = dn.op_rope(x[:5], pos[:5].contiguous(), table)
+    assert torch.equal(few, y[:5])
+
+
+def test_rope_gradient_is_the_inverse_rotation():
+    """d/dx of <g, rotate(x)> is rotate(g) at the negated position, against differences of the (linear) call."""
+    rng = np.random.default_rng(6)
+    x, xv = heads(rng, 3, 2, 16, dn.DN_FP32)
+    g, gv = heads(rng, 3, 2, 16, dn.DN_FP32)
+    pos, _ = positions(rng, 3, 1)
+    table = dn.rope_table((12,))
+    grad = host(dn.op_rope(g, -pos, table))
+    for at in ((0, 0, 0), (1, 1, 11), (2, 0, 15)):
+        e = torch.zeros_like(x)
+        e[at] = 1.0
+        diff = (gv * host(dn.op_rope(e, pos, table))).sum()
+        assert abs(diff - grad[at]) <= 40 * W * np.abs(gv).max()
+
+
+def test_values_past_the_rotated_width_pass_whole():
+    x = torch.randn(4, 3, 64, device=DEV)
+    x[..., 32:] = torch.tensor([float("inf"), float("nan"), -float("inf"), 3.0], device=DEV).repeat(8)
+    pos, _ = positions(np.random.default_rng(0), 4, 1, True)
+    for pairing in (dn.DN_ROPE_PAIRS, dn.DN_ROPE_HALVES):
+        y = dn.op_rope(x, pos, dn.rope_table((32,)), pairing=pairing)
+        assert torch.equal(torch.nan_to_num(y[..., 32:], 7.0, 8.0, 9.0), torch.nan_to_num(x[..., 32:], 7.0, 8.0, 9.0))
+        assert torch.isfinite(y[..., :32]).all()
+
+
+# ----------------------------------------------------------------------------- norm and rotation
+
+def norm_rope_ref(xv, gain, eps, pv, freqs, axes, pairing, dtype):
+    n = P.rms_norm(xv, gain, eps)
+    ref = P.rotate(n, pv, freqs, axes, pairing)
+    return ref, rope_tol(n, freqs, pairing, ref, dtype, w=24)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pairing", [dn.DN_ROPE_PAIRS, dn.DN_ROPE_HALVES])
+@pytest.mark.parametrize("dim,axes,per_axis", ROPES)
+def test_qk_norm_rope(dtype, pairing, dim, axes, per_axis):
+    for rows, hq, hk, with_v in ((1, 1, 1, False), (6, 5, 1, True), (130, 8, 2, True), (1500, 20, 4, True)):
+        announce(f"qk_norm_rope {dtype} {pairing} {dim} {rows} x {hq}, {hk}")
+        rng = np.random.default_rng(rows + dim)
+        qkv = torch.from_numpy(rng.normal(size=(rows, hq + 2 * hk, dim)).astype(np.float32) * 3).to(DEV).to(tdtype(dtype))
+        q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]
+        gq, gk = (torch.from_numpy(rng.normal(1, 0.3, dim).astype(np.float32)).to(DEV) for _ in range(2))
+        pos, pv = positions(rng, rows, len(axes))
+        table, freqs = dn.rope_table(axes, 5e5, per_axis), dn.rope_freqs(axes, 5e5, per_axis)
+        qo, ko, vo = (torch.full((rows, h, dim), 7.0, device=DEV, dtype=qkv.dtype) for h in (hq, hk, hk))
+        before = qkv.clone()
+        dn.op_qk_norm_rope(q, k, gq, gk, 1e-6, pos, table, qo, ko, v if with_v else None, vo if with_v else None, pairing=pairing)
+        assert torch.equal(qkv, before)
+        for x, g, o in ((q, gq, qo), (k, gk, ko)):
+            ref, tol = norm_rope_ref(host(x), host(g), 1e-6, pv, freqs, axes, pairing, dtype)
+            close(host(o), ref, tol)
+        assert torch.equal(vo, v if with_v else torch.full_like(vo, 7.0))
+        # in place
+        dn.op_qk_norm_rope(q, k, gq, gk, 1e-6, pos, table, q, k, pairing=pairing)
+        assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(v, before[:, hq + hk:])
+
+
+def cache_rows(q_len, kv_start, kv_len):
+    return [kv_start[s] + kv_len[s] - n + i for s, n in enumerate(q_len) for i in range(n)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("q_len", [[1], [1] * 70, [0, 3, 0, 0, 17, 1, 0], [5, 64, 2]])
+def test_qk_norm_rope_into_a_cache(dtype, q_len):
+    rng = np.random.default_rng(len(q_len))
+    dim, hq, hk, axes = 64, 4, 2, (24, 16)
+    n, total = len(q_len), sum(q_len)
+    kv_len = [m + int(rng.integers(0, 9)) for m in q_len]
+    order, at, kv_start = rng.permutation(n), 0, [0] * n
+    for s in order:                                          # sequences lie in the cache in another order, with gaps
+        at += int(rng.integers(0, 3))
+        kv_start[s] = at
+        at += kv_len[s]
+    rows = at + 5
+    extra = 3                                                # packed rows behind the last sequence
+    q, qv = heads(rng, total + extra, hq, dim, dtype)
+    k, kv = heads(rng, total + extra, hk, dim, dtype, pad=1)
+    v, vv = heads(rng, total + extra, hk, dim, dtype)
+    gain = torch.ones(dim, device=DEV)
+    pos, pv = positions(rng, total + extra, 2)
+    table, freqs = dn.rope_table(axes), dn.rope_freqs(axes)
+    qo = torch.full((total + extra, hq, dim), 7.0, device=DEV, dtype=q.dtype)
+    kc, vc = (torch.full((rows, hk, dim), 9.0, device=DEV, dtype=q.dtype) for _ in range(2))
+    seqs = dn.Sequences(int_t(np.cumsum([0] + q_len)), int_t(kv_start, torch.int64), int_t(kv_len), max(max(kv_len), 1))
+    dn.op_qk_norm_rope(q, k, gain, gain, 1e-6, pos, table, qo, kc, v, vc, seqs)
+    ref, tol = norm_rope_ref(qv, 1.0, 1e-6, pv, freqs, axes, P.PAIRS, dtype)
+    close(host(qo[:total]), ref[:total], tol[:total])
+    assert (qo[total:] == 7).all()
+    ref, tol = norm_rope_ref(kv, 1.0, 1e-6, pv, freqs, axes, P.PAIRS, dtype)
+    to = cache_rows(q_len, kv_start, kv_len)
+    close(host(kc)[to], ref[:total], tol[:total])
+    assert np.array_equal(host(vc)[to], vv[:total])
+    rest = np.setdiff1d(np.arange(rows), to)
+    assert (kc[rest] == 9).all() and (vc[rest] == 9).all()
+
+
+BAD = [  # (q_start, kv_start, kv_len) of three sequences of 4 rows in a cache of 40, the bad one
+    ([0, 4, 8, 12], [0, 37, 20], [4, 4, 4], 1), ([0, 4, 8, 12], [0, -1, 20], [4, 4, 4], 1), ([0, 4, 8, 12], [0, 10, 20], [4, -4, 4], 1),
+    ([0, 4, 8, 12], [0, 2 ** 62, 20], [4, 4, 4], 1), ([0, 4, 8, 2 ** 31 - 1], [0, 10, 20], [4, 4, 4], 2),
+    ([0, 4, 8, 12], [0, 10, 2 ** 63 - 1], [4, 4, 2 ** 31 - 1], 2), ([-5, 4, 8, 12], [0, 10, 20], [9, 4, 4], 0)]
+
+
+@pytest.mark.parametrize("q_start,kv_start,kv_len,bad", BAD)
+def test_sequences_outside_the_tensors_are_skipped(q_start, kv_start, kv_len, bad):
+    rng = np.random.default_rng(3)
+    seqs = dn.Sequences(int_t(q_start), int_t(kv_start, torch.int64), int_t(kv_len), 40)
+    q, qv = heads(rng, 12, 4, 64, dn.DN_BF16)
+    k, _ = heads(rng, 12, 2, 64, dn.DN_BF16)
+    kc, kcv = heads(rng, 40, 2, 64, dn.DN_BF16)
+    vc, vcv = heads(rng, 40, 2, 64, dn.DN_BF16)
+    good = [s for s in range(3) if s != bad]
+    o = torch.full_like(q, 7.0)
+    ws = workspace(q, kc, seqs)
+    dn.op_attention_packed(q, kc, vc, o, seqs, ws=ws)
+    for s in range(3):
+        part = host(o[4 * s:4 * s + 4])
+        if s == bad:
+            assert (part == 7).all()
+            continue
+        a = kv_start[s]
+        ref, m = P.attention(qv[4 * s:4 * s + 4], kcv[a:a + 4], vcv[a:a + 4], True, 0.125)
+        close(part, ref, 0.1 * m + 0.01)
+    gain, table, pos = torch.ones(64, device=DEV), dn.rope_table((64,)), int_t([[i] for i in range(12)])
+    before, qo = kc.clone(), torch.full_like(q, 7.0)
+    dn.op_qk_norm_rope(q, k, gain, gain, 1e-6, pos, table, qo, kc, seqs=seqs)
+    changed = {int(i) for i in (kc != before).flatten(1).any(1).nonzero()}
+    assert changed == {kv_start[s] + i for s in good for i in range(4)}
+    assert (qo[4 * bad:4 * bad + 4] == 7).all() and all((qo[4 * s:4 * s + 4] != 7).any() for s in good)
+
+
+# ----------------------------------------------------------------------------- attention
+
+def workspace(q, k, seqs):
+    return torch.full((dn.attention_packed_bytes(q, k, seqs),), 0xff, device=DEV, dtype=torch.uint8)
+
+
+class Batch:
+    """A packed batch with gaps between the sequences' key rows that hold NaN, and packed rows behind the last one."""
+
+    def __init__(self, q_len, kv_len, hq, hk, dim, dtype, seed=0, std=2.0, max_kv=None, behind=2):
+        rng = np.random.default_rng(seed)
+        self.q_len, self.kv_len, self.dtype = q_len, kv_len, dtype
+        n, at, self.start = len(q_len), 1, [0] * len(q_len)
+        for s in rng.permutation(n):
+            self.start[s] = at
+            at += kv_len[s] + int(rng.integers(0, 4))
+        self.total = sum(q_len)
+        self.q, self.qv = heads(rng, self.total + behind, hq, dim, dtype, pad=1, std=std)
+        kv = torch.full((at + 1, 2 * hk, dim), float("nan"), device=DEV, dtype=tdtype(dtype))
+        for s in range(n):
+            kv[self.start[s]:self.start[s] + kv_len[s]] = torch.from_numpy(
+                rng.normal(size=(kv_len[s], 2 * hk, dim)).astype(np.float32)).to(DEV).to(tdtype(dtype))
+        self.k, self.v = kv[:, :hk], kv[:, hk:]
+        self.o = torch.full((self.total + behind, hq, dim), 7.0, device=DEV, dtype=tdtype(dtype))
+        self.qs = np.cumsum([0] + q_len)
+        self.seqs = dn.Sequences(int_t(self.qs), int_t(self.start, torch.int64), int_t(kv_len), max_kv or max(max(kv_len), 1))
+        self.scale = dim ** -0.5
+        self.ws = workspace(self.q, self.k, self.seqs)
+
+    def run(self, causal, scale=None, stream=None):
+        dn.op_attention_packed(self.q, self.k, self.v, self.o, self.seqs, causal=causal, scale=scale, ws=self.ws, stream=stream)
+        return self.o
+
+    def check(self, causal, scale=None, rows=None):
+        got, kv, vv = host(self.o), host(self.k), host(self.v)
+        dim = kv.shape[-1]
+        scale = self.scale if scale is None else scale
+        up = U[self.dtype] if self.dtype == dn.DN_BF16 else 0.0
+        for s, (n, m) in enumerate(zip(self.q_len, self.kv_len)):
+            a, b = self.qs[s], self.start[s]
+            q, k, v = self.qv[a:a + n], kv[b:b + m], vv[b:b + m]
+            pick = np.arange(n) if rows is None else np.unique(np.clip(rows, 0, max(n - 1, 0)))[:n]
+            ref, mass = (np.zeros_like(got[a:a + n]) for _ in range(2))
+            for i in pick:
+                seen = min(m, max(0, m - n + i + 1)) if causal else m
+                ref[i], mass[i] = (t[0] for t in P.attention(q[i:i + 1], k[:seen], v[:seen], False, scale))
+            if m and n:
+                size = max(np.abs(q).sum(-1).max() * np.abs(k).max(), 1e-30) * abs(scale)
+                d = (dim + 4) * W * size + 2 * W
+            else:
+                d = 0.0
+            tol = (2 * (d + up) + (m + 4) * W) * mass + U[self.dtype] * np.abs(ref)
+            close(got[a:a + n][pick], ref[pick], tol[pick])
+        assert (self.o[self.total:] == 7).all(), "packed rows behind the last sequence"
+
+
+LENGTHS = [([1], [1]), ([1], [77]), ([63, 1, 64], [63, 1, 64]), ([65, 129, 2], [65, 130, 300]), ([0, 5, 0, 33, 0], [0, 5, 9, 64, 0]),
+           ([7, 3, 40], [3, 0, 39]), ([1] * 67, list(range(0, 134, 2)))]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hk,dim", [(2, 2, 64), (8, 2, 128), (5, 1, 64), (3, 3, 32), (8, 1, 96), (4, 2, 128)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths", range(len(LENGTHS)))
+def test_attention(dtype, hq, hk, dim, causal, lengths):
+    q_len, kv_len = LENGTHS[lengths]
+    announce(f"attention {dtype} {hq}/{hk} x {dim} {causal} {q_len[:5]} {kv_len[:5]}")
+    b = Batch(q_len, kv_len, hq, hk, dim, dtype, seed=lengths)
+    b.run(causal)
+    b.check(causal)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("q_len,kv_len,hq,hk,dim", [([700], [700], 4, 1, 128), ([513, 20], [900, 1500], 2, 2, 64),
+                                                    ([1, 1, 2], [5000, 20, 1300], 8, 2, 128), ([3], [9000], 6, 2, 64),
+                                                    ([600, 600], [600, 600], 2, 2, 128)])
+def test_attention_long(dtype, q_len, kv_len, hq, hk, dim):
+    for causal in (True, False):
+        announce(f"long attention {dtype} {q_len} {kv_len} {causal}")
+        b = Batch(q_len, kv_len, hq, hk, dim, dtype, seed=9)
+        first = b.run(causal).clone()
+        b.check(causal, rows=np.array([0, 1, 31, 32, 63, 64, 127, 128, 255, 256, 300, 511, 512, 598, 599, 698, 699]))
+        assert torch.equal(b.run(causal), first), "the same inputs, the same bits"
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,m,group", [(300, 300, 1), (1, 300, 4), (130, 1000, 2), (9, 2500, 8), (1, 20000, 1)])
+def test_every_key_counts_once(dtype, dim, n, m, group):
+    """Equal scores: a row's output is the share of its keys with every value; one key too few or too many shows."""
+    b = Batch([n], [m], group, 1, dim, dtype)
+    b.q.zero_()
+    b.qv[:] = 0
+    b.v[b.start[0]:b.start[0] + m] = 0
+    b.v[b.start[0] + torch.arange(m, device=DEV), 0, torch.arange(m, device=DEV) % dim] = 1
+    got = host(b.run(True))[:n]
+    for i in range(n):
+        seen = m - n + i + 1
+        share = np.bincount(np.arange(seen) % dim, minlength=dim) / seen
+        # p = 1 exactly; the sum is exact below 2^24 keys: one quotient and the output round
+        assert (np.abs(got[i] - share) <= (2 * W + U[dtype]) * share).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,group", [(64, 1), (128, 4), (32, 2), (96, 1)])
+def test_masked_keys_have_no_influence(dtype, dim, group):
+    """Infinities and NaN in keys and values that a row does not see (the later tokens of its own sequence) leave it alone;
+    a row that sees them gets what the formula gives."""
+    n = 150
+    b = Batch([n, 40], [n, 40], 2 * group, 2, dim, dtype, seed=2)
+    clean = host(b.run(True))
+    a = b.start[0]
+    b.k[a + 100] = float("nan")
+    b.k[a + 120, :, ::2] = float("inf")
+    b.v[a + 90, 0, :] = float("inf")
+    b.v[a + 95, 0, 3] = -float("inf")
+    b.v[a + 97, 1, 5] = float("nan")
+    got = host(b.run(True))
+    h0, h1 = slice(0, group), slice(group, 2 * group)
+    assert np.array_equal(got[:90], clean[:90]) and np.array_equal(got[n:], clean[n:])
+    assert (got[90:95, h0] == np.inf).all() and np.array_equal(got[90:97, h1], clean[90:97, h1])
+    assert np.isnan(got[95:100, h0, 3]).all() and (got[95:100, h0, 4:] == np.inf).all()
+    assert np.isnan(got[97:100, h1, 5]).all() and np.array_equal(got[97:100, h1, 6:], clean[97:100, h1, 6:])
+    assert np.isnan(got[100:n]).all()
+
+
+def test_extreme_scores():
+    """Scores of +-1e30 and equal ones at the lowest finite value: the largest take all, no NaN."""
+    b = Batch([4], [70], 1, 1, 64, dn.DN_FP32)
+    a = b.start[0]
+    b.q.fill_(1.0)
+    b.k[a:a + 70] = -1e28
+    b.k[a + 3] = 1e28
+    b.run(False, scale=1.0)
+    assert torch.allclose(b.o[:4], b.v[a + 3].expand(4, 1, 64))
+    b.k[a:a + 70] = -1e28                                      # every score -6.4e29: the mean
+    b.run(False, scale=1.0)
+    assert torch.allclose(b.o[:4], b.v[a:a + 70].mean(0).expand(4, 1, 64), atol=1e-5)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.0])
+def test_scales(scale):
+    for dtype in TYPES:
+        b = Batch([70, 1], [90, 33], 4, 2, 64, dtype, seed=4, std=1.0)
+        b.run(True, scale=scale)
+        b.check(True, scale=scale)
+
+
+@pytest.mark.parametrize("bound", [1, 100, 100000])
+def test_the_bound_of_the_lengths_decides_no_result(bound):
+    b = Batch([1, 5], [3000, 777], 8, 2, 128, dn.DN_BF16, max_kv=bound)
+    b.run(True)
+    b.check(True)
+
+
+def test_a_captured_call_follows_lengths_and_data():
+    """Capture once; replay with the lengths, keys and queries of the moment, with eager work between."""
+    b = Batch([1, 1, 1], [40, 300, 2000], 8, 2, 128, dn.DN_BF16)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        b.run(True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        b.run(True)
+    kv_len = b.seqs._keep[2]
+    for lens in ([40, 300, 2000], [39, 1, 1999], [0, 300, 64]):
+        kv_len.copy_(int_t(lens))
+        b.kv_len = lens
+        b.o.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        b.check(True)
+        replayed = b.o.clone()
+        b.ws.fill_(0xff)
+        assert torch.equal(b.run(True), replayed)
+
+
+def test_two_streams_at_once():
+    bs = [Batch([1, 3], [2500, 1200], 8, 2, 128, dn.DN_BF16, seed=s) for s in (1, 2)]
+    want = [b.run(True).clone() for b in bs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in bs]
+    for _ in range(20):
+        for b, s in zip(bs, streams):
+            b.run(True, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(b.o, w) for b, w in zip(bs, want))
+
+
+# ----------------------------------------------------------------------------- the layer
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layer_prompt_then_tokens(dtype):
+    """Norm and rotation into the cache, then attention over it, as a server runs them: a prompt in one call gives what
+    the same prompt gives in a chunk and single tokens, and both match the oracle."""
+    rng = np.random.default_rng(8)
+    dim, hq, hk, axes, lens = 64, 4, 2, (16, 24, 24), [9, 70]
+    cap, total = 96, sum(lens)
+    table, freqs = dn.rope_table(axes, 1e4), dn.rope_freqs(axes, 1e4)
+    qkv, vals = heads(rng, total, hq + 2 * hk, dim, dtype)
+    gq, gk = (torch.from_numpy(rng.normal(1, 0.2, dim).astype(np.float32)).to(DEV) for _ in range(2))
+    pos, pv = positions(rng, total, 3)
+
+    def step(rows, q_len, kv_len, kc, vc):
+        x, p = qkv[rows].contiguous(), pos[rows].contiguous()
+        q, k, v = x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+        seqs = dn.Sequences(int_t(np.cumsum([0] + q_len)), int_t([0, cap], torch.int64), int_t(kv_len), cap)
+        qo, o = (torch.empty(len(rows), hq, dim, device=DEV, dtype=x.dtype) for _ in range(2))
+        dn.op_qk_norm_rope(q, k, gq, gk, 1e-6, p, table, qo, kc, v, vc, seqs)
+        dn.op_attention_packed(qo, kc, vc, o, seqs, ws=workspace(qo, kc, seqs))
+        return o
+
+    cache = [torch.zeros(2 * cap, hk, dim, device=DEV, dtype=qkv.dtype) for _ in range(4)]
+    whole = step(list(range(total)), lens, lens, cache[0], cache[1])
+    parts = torch.empty_like(whole)
+    done = [0, 0]
+    for n in ([5, 66], [1, 1], [1, 1], [1, 1], [1, 0], [0, 1]):
+        rows = [done[0] + i for i in range(n[0])] + [lens[0] + done[1] + i for i in range(n[1])]
+        done = [done[0] + n[0], done[1] + n[1]]
+        parts[rows] = step(rows, n, done, cache[2], cache[3])
+    assert done == lens
+    assert torch.equal(cache[0], cache[2]) and torch.equal(cache[1], cache[3])
+    q = P.rotate(P.rms_norm(vals[:, :hq], host(gq), 1e-6), pv, freqs, axes, P.PAIRS)
+    k = P.rotate(P.rms_norm(vals[:, hq:hq + hk], host(gk), 1e-6), pv, freqs, axes, P.PAIRS)
+    for s, a in enumerate((0, lens[0])):
+        ref, mass = P.attention(q[a:a + lens[s]], k[a:a + lens[s]], vals[a:a + lens[s], hq + hk:], True, dim ** -0.5)
+        # q and k round by u, so a score by 2 u |q||k| scale at most; the rest as above
+        size = np.linalg.norm(q, axis=-1).max() * np.linalg.norm(k, axis=-1).max() * dim ** -0.5
+        d = 2 * U[dtype] * size + (dim + 32) * W * size * dim ** 0.5
+        tol = (2 * (d + U[dtype]) + 80 * W) * mass + U[dtype] * np.abs(ref)
+        close(host(whole[a:a + lens[s]]), ref, tol)
+        close(host(parts[a:a + lens[s]]), ref, tol)
