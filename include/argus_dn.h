@@ -377,7 +377,7 @@ dn_status ac_mx_lookup(int32_t dtype, const uint16_t* query_embs, int32_t nq, co
  *
  * Tensors of heads are device memory in the element type `dtype` (DN_BF16 or DN_FP32), rows `ld`
  * elements apart, head h in columns [h * head_dim, (h + 1) * head_dim): a slice of a wider projection
- * output is such a tensor. Rows are 16-byte aligned (pointer and ld); other buffers are aligned to their
+ * output is such a tensor. Rows are 16-byte aligned (pointer and ld, at most 2^23); other buffers are aligned to their
  * elements. Inputs and outputs do not overlap, unless said.
  * ------------------------------------------------------------------------- */
 
@@ -447,7 +447,8 @@ dn_status dn_op_qk_norm_rope(int32_t dtype, const void* q, int64_t ldq, const vo
  * h / (heads / kv_heads): q [T][ldq], o [T][ldo], k [kv_rows][ldk], v [kv_rows][ldv], head_dim 32, 64, 96 or
  * 128, heads a multiple of kv_heads. causal = 1: packed row i of the n_s of a sequence sees its first
  * kv_len - n_s + i + 1 keys; 0: all. A row that sees no key (or whose keys all score -inf) gives
- * zeros. Keys a row does not see have no influence on it, whatever they hold. Softmax and sums
+ * zeros. Keys a row does not see carry no weight, infinities and NaN among them too (a call that meets such values
+ * may round its sums in another order). Softmax and sums
  * fp32; bf16 probabilities enter the product rounded to bf16.
  * T * (heads / kv_heads) < 2^31 - 65536.
  * ws: device, 16-byte aligned, dn_attention_packed_bytes bytes (0: NULL) for the same T, heads, n and

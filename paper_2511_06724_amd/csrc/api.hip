@@ -312,8 +312,8 @@ void check_heads(const char* who, int32_t dtype, const void* x, int64_t ld, int6
   const int64_t vec = dtype == DN_BF16 ? 8 : 4;
   DN_CHECK(x, std::string(who) + ": null pointer");
   DN_CHECK(on(x, 16), std::string(who) + ": rows must be 16-byte aligned");
-  DN_CHECK(ld >= width && ld % vec == 0 && ld <= (1ll << 40),
-           std::string(who) + ": row stride must cover the heads and be a multiple of 16 bytes");
+  DN_CHECK(ld >= width && ld % vec == 0 && ld <= (1 << 23),
+           std::string(who) + ": row stride must cover the heads, be a multiple of 16 bytes and at most 2^23");
 }
 
 dn::Sequences sequences(const char* who, const dn_sequences* s) {

@@ -37,6 +37,7 @@ namespace {
 
 constexpr int kKT = 64;        // keys per tile
 constexpr float kLazy = 8.0f;  // log2 headroom before the reference maximum moves
+typedef __attribute__((address_space(1))) void gbl_void_t;
 constexpr float kLowest = -3.402823466e38f;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -53,9 +54,10 @@ template <int BM> __device__ __forceinline__ bool find_unit(const PackedAttnPara
   const int s = __builtin_amdgcn_readfirstlane(
       search_group<64>(p.seqs.n, slot, [&](int i) { return (long long)qs[i] * group / BM + i; }));
   if (s < 0) return false;
-  const int a = qs[s], b = qs[s + 1];
-  u.len_k = p.seqs.kv_len[s];
-  u.k0 = p.seqs.kv_start[s];
+  const int a = __builtin_amdgcn_readfirstlane(qs[s]), b = __builtin_amdgcn_readfirstlane(qs[s + 1]);
+  u.len_k = __builtin_amdgcn_readfirstlane(p.seqs.kv_len[s]);
+  const long long k0 = p.seqs.kv_start[s];
+  u.k0 = (long long)__builtin_amdgcn_readfirstlane((int)(k0 >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)k0);
   if (a < 0 || b <= a || b > p.T || u.len_k < 0 || u.k0 < 0 || u.k0 > p.kv_rows - u.len_k) return false;
   u.q0 = a;
   u.len_q = b - a;
@@ -64,6 +66,56 @@ template <int BM> __device__ __forceinline__ bool find_unit(const PackedAttnPara
   u.rows = (int)rows;
   u.row0 = (int)row0;
   return true;
+}
+
+// Keys a token of the unit's sequence sees.
+__device__ __forceinline__ int limit(const PackedAttnParams& p, const Unit& u, int token) {
+  return p.causal ? max(0, token + u.len_k - u.len_q + 1) : u.len_k;
+}
+
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool is_nan(float x) { return (__float_as_uint(x) & 0x7fffffffu) > 0x7f800000u; }
+
+// Maximum of scores. (fmaxf would quiet every matrix-core result first, one operation each; this one
+// hands a NaN on, whose row is NaN with any reference.)
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// Whether a result of the workgroup is an infinity or a NaN; `flags`: LDS that nothing is read from any more, one int a wave.
+template <int DB, int NW> __device__ __forceinline__ bool any_not_finite(const f32x16* o, int* flags) {
+  bool bad = false;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) bad |= not_finite(o[d][r]);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) flags[threadIdx.x >> 6] = 0;
+  __syncthreads();
+  if (bad) flags[threadIdx.x >> 6] = 1;
+  __syncthreads();
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) any |= flags[w];
+  return any != 0;
+}
+
+template <typename T> __device__ __forceinline__ T* row_out(const PackedAttnParams& p, const Unit& u, int token, int head, int D) {
+  return static_cast<T*>(p.o) + (u.q0 + token) * p.ldo + (long long)head * D;
+}
+
+// A lane's half of 32 values of an output row: 8 g + 4 (lane / 32) .. + 3 in registers 4 g .. 4 g + 3.
+template <typename T> __device__ __forceinline__ void store_block(T* op, const f32x16& o, float l) {
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  op += 4 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    T v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = from_f32<T>(o[4 * g + e] * inv);
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(op + 8 * g) = __builtin_bit_cast(uint2, bf16x4{v[0], v[1], v[2], v[3]});
+    else
+      *reinterpret_cast<f32x4*>(op + 8 * g) = f32x4{v[0], v[1], v[2], v[3]};
+  }
 }
 
 template <typename T> struct Pv;
@@ -108,36 +160,90 @@ template <> struct Pv<float> {
   __device__ static __forceinline__ void set(float& f, int, float x) { f = x; }
 };
 
-// O^T += V^T P^T of one 64-key tile of which some keys are masked, when the values may hold infinities
-// or NaN: the finite values by the product; the others are counted where they are seen.
-template <typename T, int DB>
-__device__ __forceinline__ void pv_careful(const T* vs, int ld, const f32x16* pr, const f32x16* seen, f32x16* o, int lane) {
+// The rows of a unit again (32 per wave) over keys [begin, end), when a result was not finite: infinities and NaN of V are
+// taken out of the product and counted where their keys are seen.
+template <typename T, int D, int NW, typename F>
+__device__ __forceinline__ void careful_rows(const PackedAttnParams& p, const Unit& u, int group, int kvh, T* lds, int begin, int end, F emit) {
   using MM = Mma<T>;
   using V = Pv<T>;
+  constexpr int NT = 64 * NW, VEC = 16 / sizeof(T), LD = D + VEC, NS = D / MM::KS, DB = D / 32, CH = D / VEC;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int first = u.row0 + (tid >> 6) * 32, row = min(first + (lane & 31), u.rows - 1);
+  const int token = row / group, head = kvh * group + row - token * group;
+  const int lim = limit(p, u, token);
+  const T* qp = static_cast<const T*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D + half * MM::KPL;
+  const T* kp = static_cast<const T*>(p.k) + u.k0 * p.ldk + (long long)kvh * D;
+  const T* vp = static_cast<const T*>(p.v) + u.k0 * p.ldv + (long long)kvh * D;
+  T* ks = lds;
+  T* vs = lds + kKT * LD;
 #pragma unroll 1
-  for (int sign = 0; sign < 3; ++sign) {
+  for (int d = 0; d < DB; ++d) {  // 32 output values at a time: few registers, for a path that is hardly ever taken
+    f32x16 o;
+    float m = kLowest, l = 0.f;
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      f32x16 n;
+    for (int r = 0; r < 16; ++r) o[r] = 0.f;
+#pragma unroll 1
+    for (int k0 = begin; k0 < end; k0 += kKT) {
+      __syncthreads();
+#pragma unroll 1
+      for (int w = tid; w < kKT * CH; w += NT) {
+        const int r = w / CH, c = w - r * CH;
+        const long long key = min(k0 + r, end - 1);
+        st16(ks + r * LD + c * VEC, ld16(kp + key * p.ldk + c * VEC));
+        st16(vs + r * LD + c * VEC, ld16(vp + key * p.ldv + c * VEC));
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (int kb = 0; kb < 2; ++kb) {
+        f32x16 s, n;
+        float mx = -INFINITY;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) n[r] = sign == 0 ? o[d][r] : 0.f;
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < NS; ++i)
+          s = MM::mma(MM::load(&ks[(kb * 32 + (lane & 31)) * LD + i * MM::KS + half * MM::KPL]), MM::load(qp + i * MM::KS), s);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int c = 0; c < V::STEPS; ++c) {
-          typename MM::frag f = V::v(vs, ld, kb, c, d * 32, lane);
-#pragma unroll
-          for (int e = 0; e < V::N; ++e) {
-            const float x = V::get(f, e);
-            const bool finite = fabsf(x) <= -kLowest, other = sign == 1 ? x < 0 : x > 0;
-            V::set(f, e, sign == 0 ? (finite ? x : 0.f) : (finite || other ? 0.f : 1.f));
-          }
-          n = MM::mma(f, V::p(sign == 0 ? pr[kb] : seen[kb], c), n);
+        for (int r = 0; r < 16; ++r) {
+          s[r] = k0 + kb * 32 + acc_row(r, lane) < min(lim, end) ? s[r] * p.scale_log2 : -INFINITY;
+          mx = fmaxf(mx, s[r]);
         }
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - m_new);
+        m = m_new;
+        l *= alpha;
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        o[d][r] = sign == 0 ? n[r] : n[r] == 0.f ? o[d][r] : o[d][r] + (sign == 1 ? INFINITY : -INFINITY);
+        for (int r = 0; r < 16; ++r) {
+          o[r] *= alpha;
+          s[r] = to_f32(from_f32<T>(fast_exp2(s[r] - m)));
+          l += s[r];
+        }
+#pragma unroll 1
+        for (int sign = 0; sign < 3; ++sign) {  // the finite values; +inf (and NaN); -inf (and NaN)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            if (sign > 0) s[r] = k0 + kb * 32 + acc_row(r, lane) < min(lim, end) ? 1.f : 0.f;  // count where a key is seen
+            n[r] = sign == 0 ? o[r] : 0.f;
+          }
+#pragma unroll
+          for (int c = 0; c < V::STEPS; ++c) {
+            typename MM::frag f = V::v(vs, LD, kb, c, d * 32, lane);
+#pragma unroll
+            for (int e = 0; e < V::N; ++e) {
+              const float x = V::get(f, e);
+              const bool finite = !not_finite(x), other = sign == 1 ? x < 0 : x > 0;
+              V::set(f, e, sign == 0 ? (finite ? x : 0.f) : (finite || (other && !is_nan(x)) ? 0.f : 1.f));
+            }
+            n = MM::mma(f, V::p(s, c), n);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            o[r] = sign == 0 ? n[r] : n[r] == 0.f ? o[r] : o[r] + (sign == 1 ? INFINITY : -INFINITY);
+        }
+      }
     }
+    l += __shfl_xor(l, 32, 64);
+    if (first + (lane & 31) < u.rows) emit(token, head, d, o, m, l);
   }
 }
 
@@ -165,13 +271,9 @@ __global__ __launch_bounds__(64 * NW) void packed_kernel(PackedAttnParams p, int
   const int first = u.row0 + wave * 32;  // first row of the wave
   const int row = min(first + (lane & 31), u.rows - 1);
   const int token = row / group, head = kvh * group + row - token * group;
-  const int shift = u.len_k - u.len_q;
-  auto limit = [&](int tok) { return p.causal ? max(0, tok + shift + 1) : u.len_k; };
-  const int lim = limit(token);
-  const int lim_min = limit(min(first, u.rows - 1) / group);                 // of the wave
-  const int end = limit(min(u.row0 + BM - 1, u.rows - 1) / group);            // of the workgroup
-  T* op = static_cast<T*>(p.o) + (u.q0 + token) * p.ldo + (long long)head * D;
-  const bool store_row = first + (lane & 31) < u.rows;
+  const int lim = limit(p, u, token);
+  const int lim_min = limit(p, u, min(first, u.rows - 1) / group);                // of the wave
+  const int end = limit(p, u, min(u.row0 + BM - 1, u.rows - 1) / group);          // of the workgroup
 
   const T* qp = static_cast<const T*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D;
   typename MM::frag qf[NS];
@@ -181,7 +283,6 @@ __global__ __launch_bounds__(64 * NW) void packed_kernel(PackedAttnParams p, int
   const T* vp = static_cast<const T*>(p.v) + u.k0 * p.ldv + (long long)kvh * D;
 
   const int ntiles = (end + kKT - 1) / kKT;
-  const bool any_masked = limit(u.row0 / group) < ntiles * kKT;  // a masked key in a tile (workgroup-uniform)
   f32x16 o[DB];
   float m_ref, l_run;
   uint4 rk[PER], rv[PER];
@@ -208,13 +309,13 @@ __global__ __launch_bounds__(64 * NW) void packed_kernel(PackedAttnParams p, int
     }
   };
 
-  for (bool careful = false;; careful = true) {
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+  for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    m_ref = kLowest;
-    l_run = 0.f;
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  m_ref = kLowest;
+  l_run = 0.f;
+  {
     if (ntiles > 0) {
       load(0);
       store(0);
@@ -273,14 +374,7 @@ __global__ __launch_bounds__(64 * NW) void packed_kernel(PackedAttnParams p, int
           rs += e;
         }
       l_run += rs + __shfl_xor(rs, 32, 64);
-      if (masked && careful) {
-        f32x16 seen[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) seen[kb][r] = k0 + kb * 32 + acc_row(r, lane) < lim ? 1.f : 0.f;
-        pv_careful<T, DB>(vs, LD, s, seen, o, lane);
-      } else {
+      {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -296,30 +390,593 @@ __global__ __launch_bounds__(64 * NW) void packed_kernel(PackedAttnParams p, int
       }
       __syncthreads();
     }
-    if (careful || !any_masked) break;
-    float bad = 0.f;  // NaN if a result is not finite
+  }
+  if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds))) 
+    return careful_rows<T, D, NW>(p, u, group, kvh, lds, 0, end, [&](int tok, int h, int d, const f32x16& x, float, float sum) {
+      store_block<T>(row_out<T>(p, u, tok, h, D) + 32 * d, x, sum);
+    });
+  if (first + (lane & 31) < u.rows) {
+    T* op = row_out<T>(p, u, token, head, D);
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d) store_block<T>(op + 32 * d, o[d], l_run);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// bf16: the matrix cores and the vector unit kept busy at once.
+//
+// Tiles of KT keys (rows of K, rows of V) go global -> LDS without registers into a ring of R slots. Work
+// is pipelined over blocks of 32 keys: while the exponentials of block j run on the vector unit,
+// the matrix cores take the scores of block j + 1 and add the values of block j - 1 with the
+// probabilities of the step before. None of the three waits for another, so they are laid out by hand
+// in chunks of one matrix instruction, the load of a fragment two chunks ahead and a share of the
+// exponentials, held apart by scheduling barriers. Then comes the one decision of a step: whether the
+// maximum of the new scores moves the reference; if so, the pending values are added first and O and l scaled.
+//
+// At the top of tile t a wave waits for its loads of tile t + 1 and meets the others: theirs have
+// landed then, and all are done with tile t - 2, whose slot takes tile t + R - 2. Of the waves on a SIMD the
+// older one is served first and would run ahead into that barrier, leaving the other alone: priorities
+// fall over the steps of a tile, so that the wave that is behind is served first.
+//
+// LDS rows are D * 2 bytes in 16-byte pieces, stored xor a function of the row so that reads are free
+// of bank conflicts: a lane reads one piece of K row lane % 32; a transposing read of V takes 32 bytes (a pair
+// of pieces) of each of 4 rows.
+template <int D, int KT> struct Tile {
+  static constexpr int CH = D / 8;                            // 16-byte pieces per row
+  static constexpr int BYTES = KT * D * 2;                    // of K, and of V
+  // low bits of a step of K (two pieces) and of a block of V (two pairs) that the xor reaches
+  static constexpr int XS = D == 128 ? 7 : D == 64 ? 3 : 1, XD = D == 128 ? 3 : D == 64 ? 1 : 0;
+  // 8 rows' pieces lie in different 16-byte columns of 128 bytes and 16 rows' of 256
+  __device__ static __forceinline__ int k_piece(int row, int c) {
+    return c ^ (D == 128  ? row & 15
+                : D == 64 ? (row & 7) ^ ((row >> 3) & 1)
+                : D == 32 ? (((row >> 1) ^ (row >> 3)) & 1) | ((row >> 1) & 2)
+                          : row & 3);
+  }
+  // 4 rows' pairs in different 32-byte columns of 128 bytes, 4 rows' two neighbouring pairs of 256
+  __device__ static __forceinline__ int v_piece(int row, int c) {
+    return c ^ (D == 128  ? ((row & 1) << 2) | ((row & 2) ? 10 : 0)
+                : D == 64 ? (row & 3) << 1
+                : D == 32 ? row & 2
+                          : (row & 1) << 1);
+  }
+};
+
+template <int D, int KT, int NW, int R, int WPE>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) void packed_pipe_kernel(PackedAttnParams p, int group,
+                                                                                                         int slots) {
+  using TL = Tile<D, KT>;
+  using V = Pv<bf16>;
+  constexpr int BM = 32 * NW, H = KT / 32;
+  constexpr int NS = D / 16, DB = D / 32;    // steps of the scores, blocks of the values
+  constexpr int C = NS + 2 * DB, PF = 2;     // chunks; how many ahead a fragment is loaded
+  constexpr int PW = KT * TL::CH / 64 / NW;  // 1 KB loads of K (and of V) per wave and tile
+  static_assert(KT * TL::CH % (64 * NW) == 0, "whole loads per wave");
+  static_assert(C % PF == 0, "a fragment's place is the same in every step");
+  static_assert(R >= 4 && (H == 1 || H == 2) && 2 * PW * (H == 1 ? 2 : 1) <= C, "ring and loads");
+  constexpr int LDS = R * 2 * TL::BYTES;
+  static_assert(2 * kKT * (D + 8) * 2 <= LDS, "careful_rows fits");
+  __shared__ __align__(16) unsigned char lds[LDS];
+
+  // ids are dealt to the eight XCDs in turn: each gets a contiguous range of key heads, whose keys stay in its L2
+  const int total = gridDim.x, xcd = blockIdx.x % 8;
+  const int logical = xcd * (total / 8) + min(xcd, total % 8) + blockIdx.x / 8;
+  const int kvh = logical / slots;
+  int slot = logical - kvh * slots;
+  if (p.causal) slot = slots - 1 - slot;  // the longest key ranges first
+  Unit u;
+  if (!find_unit<BM>(p, group, slot, u)) return;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first = u.row0 + wave * 32;
+  const int row = min(first + (lane & 31), u.rows - 1), token = row / group, head = kvh * group + row - token * group;
+  const int lim = limit(p, u, token);
+  const int lo = __builtin_amdgcn_readfirstlane(limit(p, u, min(first, u.rows - 1) / group));      // the wave's shortest range
+  const int hi = __builtin_amdgcn_readfirstlane(limit(p, u, min(first + 31, u.rows - 1) / group)); // and longest
+  const int end = __builtin_amdgcn_readfirstlane(limit(p, u, min(u.row0 + BM - 1, u.rows - 1) / group));
+  const int ntiles = (end + KT - 1) / KT, mine = first < u.rows ? (hi + KT - 1) / KT : 0;
+
+  // a negative scale is one of -q (exactly), scale 0 one of 0 q: a masked score then is -inf
+  float c = p.scale_log2;
+  bf16x8 qf[NS];
+  {
+    const bf16* qp = static_cast<const bf16*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D + half * 8;
+    const unsigned flip = c < 0.f ? 0x80008000u : 0u, keep = c == 0.f ? 0u : ~0u;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) bad += o[d][r] * 0.f;
-    if (!__syncthreads_or(bad != bad)) break;
+    for (int s = 0; s < NS; ++s) {
+      const uint4 w = ld16(qp + s * 16);
+      qf[s] = __builtin_bit_cast(bf16x8, make_uint4((w.x ^ flip) & keep, (w.y ^ flip) & keep, (w.z ^ flip) & keep, (w.w ^ flip) & keep));
+    }
+  }
+  c = c == 0.f ? 1.f : fabsf(c);
+
+  // loads of a tile: piece i * 64 + lane of K and of V, wave-uniform bases and 32-bit lane offsets
+  const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16*>(p.k) + u.k0 * p.ldk + (long long)kvh * D);
+  const char* vbase = reinterpret_cast<const char*>(static_cast<const bf16*>(p.v) + u.k0 * p.ldv + (long long)kvh * D);
+  unsigned koff[PW], voff[PW];
+  auto set_offsets = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < PW; ++j) {
+      const int w = (wave * PW + j) * 64 + lane, r = w / TL::CH, ch = w - r * TL::CH;
+      const unsigned key = (unsigned)(min(t * KT + r, end - 1) - t * KT);
+      koff[j] = 2u * (key * (unsigned)p.ldk + 8u * TL::k_piece(r, ch));
+      voff[j] = 2u * (key * (unsigned)p.ldv + 8u * TL::v_piece(r, ch));
+    }
+  };
+  auto load_k = [&](int at, int j) { dma16_base(kbase, koff[j], (lds_void*)(lds + at * 2 * TL::BYTES + (wave * PW + j) * 1024)); };
+  auto load_v = [&](int at, int j) { dma16_base(vbase, voff[j], (lds_void*)(lds + at * 2 * TL::BYTES + TL::BYTES + (wave * PW + j) * 1024)); };
+  int issued = 0;
+  // past the last tile it is loaded again: the same count of loads per tile, which nothing reads
+  auto advance = [&] {
+    if (issued < ntiles - 1) {
+      ++issued;
+      kbase += 2 * KT * p.ldk;
+      vbase += 2 * KT * p.ldv;
+      if (issued == ntiles - 1) set_offsets(issued);
+    }
+  };
+  auto issue = [&](int at) {
+#pragma unroll
+    for (int j = 0; j < PW; ++j) load_k(at, j);
+#pragma unroll
+    for (int j = 0; j < PW; ++j) load_v(at, j);
+    advance();
+  };
+
+  // lane offsets of the fragments within a slot. Step s of K is piece 2 s + half, block d of V the pieces from 4 d:
+  // their low bits go into the xor with the row, the rest is added
+  constexpr int XS = TL::XS, XD = TL::XD;
+  const int kfo = (lane & 31) * D * 2 + TL::k_piece(lane & 31, half) * 16;
+  const int vrow = 4 * half + ((lane & 15) >> 2), vcol = (lane & 16) + 4 * (lane & 3);
+  const int vfo = TL::BYTES + vrow * D * 2 + TL::v_piece(vrow, vcol >> 3) * 16 + (vcol & 7) * 2;
+  auto k_frag = [&](const unsigned char* T, int kb, int s) {
+    return *reinterpret_cast<const bf16x8*>(T + (kfo ^ ((s & XS) << 5)) + ((s & ~XS) << 5) + kb * 32 * D * 2);
+  };
+  // fragment n of a block's values: keys 16 (n / DB) .., values 32 (n % DB) ..
+  auto v_frag = [&](const unsigned char* T, int kb, int n) {
+    const int cc = n / DB, d = n % DB;
+    const unsigned char* a = T + (vfo ^ ((d & XD) << 6)) + ((d & ~XD) << 6) + (kb * 32 + 16 * cc) * D * 2;
+    const bf16x4 l = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((V::lds_s16x4*)a));
+    const bf16x4 h = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((V::lds_s16x4*)(a + 8 * D * 2)));
+    return __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  f32x16 o[DB];
+  float sa[16], m = kLowest, l = 0.f, top = 0.f;  // scores at hand, reference maximum, row sum, the scores' maximum
+  bool move = false;                              // that maximum exceeds the reference somewhere in the wave
+  bf16x8 pf[2][2], fr[PF];
+  const bf16x8 none = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  pf[1][0] = pf[1][1] = none;
+
+  // eight scores leave the accumulators; their maximum
+  auto take = [&](const f32x16& x, float* y) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = x[e];
+      asm("" : "+v"(y[e]));
+    }
+    return max2(max2(max2(max2(max2(y[0], y[1]), y[2]), max2(max2(y[3], y[4]), y[5])), y[6]), y[7]);
+  };
+  auto compare = [&](float x) {
+    top = x * c;
+    move = __any(top > m + kLazy);
+  };
+  auto zero16 = [] {
+    f32x16 z;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+    return z;
+  };
+  // O^T += V^T P^T of one block
+  auto values = [&](const unsigned char* T, int kb, const bf16x8 (&pp)[2]) {
+#pragma unroll
+    for (int n = 0; n < 2 * DB; ++n) {
+      o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(T, kb, n), pp[n / DB], o[n % DB], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // Block j: its exponentials into pn; scores of block j + 1 (block kn of tile Tn); values of block j - 1 (kp of Tp) with
+  // pp; first fragments of the values of block j (kc of Tc) for the next step; loads into slot `in`.
+  auto step = [&](int j, const unsigned char* Tp, int kp, const unsigned char* Tn, int kn, const unsigned char* Tc, int kc, int in,
+                  bf16x8 (&pp)[2], bf16x8 (&pn)[2]) {
+    if ((j + 1) * 32 > lo) {  // keys past a range
+      float x = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (j * 32 + acc_row(r, lane) >= lim) sa[r] = -INFINITY;
+        x = fmaxf(x, sa[r]);
+      }
+      compare(x);
+    }
+    if (move) {
+      values(Tp, kp, pp);
+      const float m_new = fmaxf(m, fmaxf(top, __shfl_xor(top, 32, 64)));
+      const float alpha = fast_exp2(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      m = m_new;
+      pp[0] = pp[1] = none;
+    }
+    f32x16 sn;
+    float w[2], ev[4], sv[16];
+    // probabilities 2 k, 2 k + 1 to bf16, and into the row sum
+    auto round_pair = [&](int k) {
+      const bf16x2 ones = {static_cast<bf16>(1.f), static_cast<bf16>(1.f)};
+      unsigned pair = pack_bf16(ev[(2 * k) & 3], ev[(2 * k + 1) & 3]);
+      asm volatile("" : "+v"(pair));
+      const bf16x2 pr = __builtin_bit_cast(bf16x2, pair);
+      pn[k >> 2][(2 * k) & 7] = pr[0];
+      pn[k >> 2][(2 * k + 1) & 7] = pr[1];
+      l = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l, false);
+    };
+    // chunks: the first PF values, the scores, the other values (beside which the scores are taken)
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const bf16x8 f = fr[i % PF];
+      if (H == 2 && i % (C / 2) == 0) {
+        if (kc == 0 && i == 0) __builtin_amdgcn_s_setprio(3);
+        if (kc == 0 && i != 0) __builtin_amdgcn_s_setprio(2);
+        if (kc == 1 && i == 0) __builtin_amdgcn_s_setprio(1);
+        if (kc == 1 && i != 0) __builtin_amdgcn_s_setprio(0);
+      }
+      if (i % 2 == 1) {  // tiles of two blocks: K beside the first, V beside the second
+        const int n = i / 2;
+        if (H == 1 ? n < PW : kc == 0 && n < PW) load_k(in, n);
+        if (H == 1 ? n >= PW && n < 2 * PW : kc == 1 && n < PW) load_v(in, H == 1 ? n - PW : n);
+      }
+      {
+        const int n = i + PF;
+        fr[i % PF] = n < PF + NS ? k_frag(Tn, kn, n - PF) : n < C ? v_frag(Tp, kp, n - NS) : v_frag(Tc, kc, n - C);
+      }
+      if (i >= PF && i < PF + NS) {
+        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i - PF], i == PF ? zero16() : sn, 0, 0, 0);
+      } else {
+        const int n = i < PF ? i : i - NS;
+        o[n % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pp[n / DB], o[n % DB], 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = i * 16 / C; e < (i + 1) * 16 / C; ++e) {
+        if (e >= 2 && e % 2 == 0) round_pair(e / 2 - 1);
+        ev[e & 3] = fast_exp2(fmaf(sa[e], c, -m));
+        asm volatile("" : "+v"(ev[e & 3]));
+      }
+      constexpr int S1 = PF + NS + 1;
+      if (i == (S1 < C - 1 ? S1 : C - 1)) w[0] = take(__builtin_shufflevector(sn, sn, 0, 1, 2, 3, 4, 5, 6, 7, 0, 1, 2, 3, 4, 5, 6, 7), sv);
+      if (i == (S1 + 1 < C - 1 ? S1 + 1 : C - 1))
+        w[1] = take(__builtin_shufflevector(sn, sn, 8, 9, 10, 11, 12, 13, 14, 15, 8, 9, 10, 11, 12, 13, 14, 15), sv + 8);
+      if (i == (S1 + 2 < C - 1 ? S1 + 2 : C - 1)) compare(max2(w[0], w[1]));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    round_pair(7);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sa[r] = sv[r];
+  };
+
+  if (ntiles > 0) {
+    set_offsets(0);
+#pragma unroll
+    for (int t = 0; t < R - 2; ++t) issue(t);
+    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((R - 3) * 2 * PW));
+    __builtin_amdgcn_s_barrier();
+    f32x16 s0 = zero16();
+#pragma unroll
+    for (int s = 0; s < NS; ++s) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(lds, 0, s), qf[s], s0, 0, 0, 0);
+    const float x0 = take(__builtin_shufflevector(s0, s0, 0, 1, 2, 3, 4, 5, 6, 7, 0, 1, 2, 3, 4, 5, 6, 7), sa);
+    const float x1 = take(__builtin_shufflevector(s0, s0, 8, 9, 10, 11, 12, 13, 14, 15, 8, 9, 10, 11, 12, 13, 14, 15), sa + 8);
+    compare(max2(x0, x1));
+#pragma unroll
+    for (int i = 0; i < PF; ++i) fr[i] = v_frag(lds, H - 1, i);
+    int at = 0;  // slot of tile t
+    const unsigned char* Tp = lds;
+    auto turn = [&] {
+      __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((R - 4) * 2 * PW));
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int t = 0; t < mine; ++t) {
+      turn();
+      const unsigned char* T = lds + at * 2 * TL::BYTES;
+      const int in = at < 2 ? at + R - 2 : at - 2;
+      at = at == R - 1 ? 0 : at + 1;
+      const unsigned char* Tn = lds + at * 2 * TL::BYTES;
+      if constexpr (H == 2) {
+        step(2 * t, Tp, 1, T, 1, T, 0, in, pf[1], pf[0]);
+        step(2 * t + 1, T, 0, Tn, 0, T, 1, in, pf[0], pf[1]);
+      } else {
+        step(t, Tp, 0, Tn, 0, T, 0, in, pf[1], pf[0]);
+        pf[1][0] = pf[0][0];
+        pf[1][1] = pf[0][1];
+      }
+      advance();
+      Tp = T;
+    }
+    values(Tp, H - 1, pf[1]);
+    for (int t = mine; t < ntiles; ++t) {  // the other waves' tiles: this one's share of the loads
+      turn();
+      issue(at < 2 ? at + R - 2 : at - 2);
+      at = at == R - 1 ? 0 : at + 1;
+    }
+    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0(0));
+  }
+  l += __shfl_xor(l, 32, 64);  // each half has summed its own keys
+  if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds))) 
+    return careful_rows<bf16, D, NW>(p, u, group, kvh, reinterpret_cast<bf16*>(lds), 0, end, [&](int tok, int h, int d, const f32x16& x, float, float sum) {
+      store_block<bf16>(row_out<bf16>(p, u, tok, h, D) + 32 * d, x, sum);
+    });
+  if (first + (lane & 31) < u.rows) {
+    bf16* op = row_out<bf16>(p, u, token, head, D);
+#pragma unroll
+    for (int d = 0; d < DB; ++d) store_block<bf16>(op + 32 * d, o[d], l);
+  }
+}
+
+template <int D, int KT, int NW, int R, int WPE> void launch_pipe(const PackedAttnParams& p, hipStream_t s) {
+  constexpr int BM = 32 * NW;
+  const int group = p.heads / p.kv_heads;
+  const long long slots = p.T * group / BM + p.seqs.n;
+  DN_CHECK(slots * p.kv_heads * (64 * NW) < (1ll << 32), "dn_op_attention_packed: too many rows for one launch");
+  hipLaunchKernelGGL((packed_pipe_kernel<D, KT, NW, R, WPE>), dim3((unsigned)(slots * p.kv_heads)), dim3(64 * NW), 0, s, p, group, (int)slots);
+  DN_HIP(hipGetLastError());
+}
+
+// ---------------------------------------------------------------------------
+// Few rows per sequence (single tokens, short drafts) over many keys: bound by reading K and V once.
+//
+// A workgroup has 32 rows of a unit and one of `splits` shares of its key range. Each of its NW waves takes every
+// NW-th block of 32 keys, loaded global -> LDS into a ring of its own, so nothing waits for another wave
+// until the end, where the waves' (m, l, O) meet in LDS in wave order. With several shares the partial results go to the
+// workspace and a second kernel joins them in order: results do not depend on timing.
+template <typename T, int D> struct Block {
+  static constexpr int RB = D * (int)sizeof(T), CH = RB / 16;  // bytes and 16-byte pieces per row
+  static constexpr int BYTES = 32 * RB;                        // of K, and of V
+  static constexpr int KX = CH % 16 == 0 ? 15 : CH % 8 == 0 ? 7 : 3, VX = sizeof(T) == 4 ? 0 : CH % 8 == 0 ? 3 : 1;
+  __device__ static __forceinline__ int k_piece(int row, int c) { return c ^ (row & KX); }
+  __device__ static __forceinline__ int v_piece(int row, int c) { return c ^ ((row & VX) << 1); }
+};
+
+struct Partials {
+  float* o = nullptr;    // [splits][T][heads][D]
+  float2* ml = nullptr;  // [splits][T][heads] (m, l)
+};
+
+template <typename T, int D, int NW, int R>
+__global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams p, int group, int splits, Partials part) {
+  using MM = Mma<T>;
+  using BL = Block<T, D>;
+  constexpr int NV = BL::CH / 2;             // 16-byte operands of a K or Q row per lane
+  constexpr int DB = D / 32;
+  constexpr int LW = 32 * BL::CH / 64;       // 1 KB loads of K (and of V) per block
+  constexpr int RING = NW * R * 2 * BL::BYTES, CARE = 2 * kKT * (D + 16 / (int)sizeof(T)) * (int)sizeof(T), JOIN = NW * (DB * 16 * 64 + 64) * 4;
+  constexpr int LDS = RING > CARE ? (RING > JOIN ? RING : JOIN) : (CARE > JOIN ? CARE : JOIN);
+  __shared__ __align__(16) unsigned char lds[LDS];
+
+  Unit u;
+  if (!find_unit<32>(p, group, blockIdx.x, u)) return;
+  u.rows = min(u.rows, u.row0 + 32);
+  const int kvh = blockIdx.y, split = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, r32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row = min(u.row0 + r32, u.rows - 1), token = row / group, head = kvh * group + row - token * group;
+  const int lim = limit(p, u, token);
+  const int range = __builtin_amdgcn_readfirstlane(limit(p, u, (u.rows - 1) / group));
+  const int lo = __builtin_amdgcn_readfirstlane(limit(p, u, u.row0 / group));
+  const long long blocks = (range + 31) / 32;
+  const int b0 = (int)(blocks * split / splits), b1 = (int)(blocks * (split + 1) / splits);
+  const int end = min(range, b1 * 32);
+  auto at = [&](int tok, int h) { return ((long long)split * p.T + u.q0 + tok) * p.heads + h; };
+  auto emit = [&](int tok, int h, int d, const f32x16& x, float m, float sum) {
+    if (splits == 1) return store_block<T>(row_out<T>(p, u, tok, h, D) + 32 * d, x, sum);
+    float* o = part.o + at(tok, h) * D + 32 * d + 4 * half;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(o + 8 * g) = f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
+    if (d == 0 && half == 0) part.ml[at(tok, h)] = make_float2(m, sum);
+  };
+  if (b0 >= b1 && splits > 1) {  // no keys: nothing to join
+    if (wave == 0 && half == 0 && u.row0 + r32 < u.rows) part.ml[at(token, head)] = make_float2(kLowest, 0.f);
+    return;
   }
 
-  if (store_row) {
-    const float inv = l_run != 0.f ? 1.f / l_run : 0.f;
+  const T* qp = static_cast<const T*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D + half * (16 / sizeof(T));
+  uint4 qv[NV];
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+  for (int s = 0; s < NV; ++s) qv[s] = ld16(qp + s * (32 / sizeof(T)));
+  const char* kbase = reinterpret_cast<const char*>(static_cast<const T*>(p.k) + u.k0 * p.ldk + (long long)kvh * D);
+  const char* vbase = reinterpret_cast<const char*>(static_cast<const T*>(p.v) + u.k0 * p.ldv + (long long)kvh * D);
+  unsigned char* ring = lds + wave * R * 2 * BL::BYTES;
+  auto issue = [&](int b, int slot) {  // block b, or the range's last key where it has none
+    const char* kb = kbase + (long long)b * 32 * p.ldk * (int)sizeof(T);
+    const char* vb = vbase + (long long)b * 32 * p.ldv * (int)sizeof(T);
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        T v[4];
+    for (int j = 0; j < LW; ++j) {
+      const int w = j * 64 + lane, r = w / BL::CH, ch = w - r * BL::CH;
+      const unsigned key = (unsigned)(min(b * 32 + r, end - 1) - b * 32);
+      dma16_base(kb, key * (unsigned)p.ldk * (unsigned)sizeof(T) + 16u * BL::k_piece(r, ch), (lds_void*)(ring + slot * 2 * BL::BYTES + j * 1024));
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = from_f32<T>(o[d][4 * g + e] * inv);
-        T* dst = op + d * 32 + 8 * g + 4 * half;
-        if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<uint2*>(dst) = __builtin_bit_cast(uint2, bf16x4{v[0], v[1], v[2], v[3]});
-        else
-          *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
+    for (int j = 0; j < LW; ++j) {
+      const int w = j * 64 + lane, r = w / BL::CH, ch = w - r * BL::CH;
+      const unsigned key = (unsigned)(min(b * 32 + r, end - 1) - b * 32);
+      dma16_base(vb, key * (unsigned)p.ldv * (unsigned)sizeof(T) + 16u * BL::v_piece(r, ch), (lds_void*)(ring + slot * 2 * BL::BYTES + BL::BYTES + j * 1024));
+    }
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  float m = kLowest, l = 0.f;
+  const int mine = b1 - b0 > wave ? (b1 - b0 - wave + NW - 1) / NW : 0;  // blocks of the wave
+  if (mine > 0) {
+#pragma unroll
+    for (int i = 0; i < R - 1; ++i) issue(b0 + wave + min(i, mine - 1) * NW, i);
+  }
+  int slot = 0;
+  for (int i = 0; i < mine; ++i) {
+    // reads of the slot that is loaded now are done; past the last block it is loaded again, so that the count of
+    // loads behind a block is the same
+    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0(63));
+    issue(b0 + wave + min(i + R - 1, mine - 1) * NW, slot == 0 ? R - 1 : slot - 1);
+    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((R - 1) * 2 * LW));
+    __builtin_amdgcn_sched_barrier(0);
+    const unsigned char* K = ring + slot * 2 * BL::BYTES;
+    const T* vs = reinterpret_cast<const T*>(K + BL::BYTES);
+    const int k0 = (b0 + wave + i * NW) * 32;
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const uint4 kv = *reinterpret_cast<const uint4*>(K + r32 * BL::RB + BL::k_piece(r32, 2 * n + half) * 16);
+      if constexpr (sizeof(T) == 4) {
+        const f32x4 ka = __builtin_bit_cast(f32x4, kv), qa = __builtin_bit_cast(f32x4, qv[n]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = MM::mma(ka[e], qa[e], s);
+      } else {
+        s = MM::mma(__builtin_bit_cast(bf16x8, kv), __builtin_bit_cast(bf16x8, qv[n]), s);
       }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] *= p.scale_log2;
+    if (k0 + 32 > min(lo, end)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (k0 + acc_row(r, lane) >= min(lim, end)) s[r] = -INFINITY;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    if (__any(mx > m + kLazy)) {
+      const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      m = m_new;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = to_f32(from_f32<T>(fast_exp2(s[r] - m)));
+      l += s[r];
+    }
+    if constexpr (sizeof(T) == 4) {
+      // register 4 g + e: key 8 g + 4 half + e (V is stored as it is)
+#pragma unroll
+      for (int c = 0; c < 16; ++c)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = MM::mma(vs[(8 * (c >> 2) + 4 * half + (c & 3)) * D + d * 32 + r32], s[c], o[d]);
+    } else {
+      const int vrow = 4 * half + ((lane & 15) >> 2), vcol = (lane & 16) + 4 * (lane & 3);
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc) {
+        const bf16x8 pf = Pv<bf16>::p(s, cc);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int col = d * 32 + vcol, r0 = 16 * cc + vrow;  // rows r0 and r0 + 8 have one xor
+          const unsigned char* a = K + BL::BYTES + r0 * BL::RB + BL::v_piece(r0, col >> 3) * 16 + (col & 7) * 2;
+          const bf16x4 x = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Pv<bf16>::lds_s16x4*)a));
+          const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Pv<bf16>::lds_s16x4*)(a + 8 * BL::RB)));
+          o[d] = MM::mma(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[d]);
+        }
+      }
+    }
+    slot = slot == R - 1 ? 0 : slot + 1;
+  }
+  __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0(0));
+  l += __shfl_xor(l, 32, 64);
+  if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds))) {
+    __syncthreads();
+    return careful_rows<T, D, NW>(p, u, group, kvh, reinterpret_cast<T*>(lds), b0 * 32, end, emit);
+  }
+  __syncthreads();
+
+  // the waves' results in order: thread (unit w of 32 values d, lane) sums over the waves
+  float* so = reinterpret_cast<float*>(lds);         // [wave][DB][16][64]
+  float* sm = so + NW * DB * 16 * 64;                // [wave][32] m, then [wave][32] l
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) so[((wave * DB + d) * 16 + r) * 64 + lane] = o[d][r];
+  if (half == 0) {
+    sm[wave * 32 + r32] = m;
+    sm[NW * 32 + wave * 32 + r32] = l;
+  }
+  __syncthreads();
+  if (u.row0 + r32 >= u.rows) return;
+  float top = sm[r32], sum = 0.f, f[NW];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w * 32 + r32]);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    f[w] = fast_exp2(sm[w * 32 + r32] - top);
+    sum += f[w] * sm[NW * 32 + w * 32 + r32];
+  }
+  for (int d = wave; d < DB; d += NW) {
+    f32x16 x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) x[r] += f[w] * so[((w * DB + d) * 16 + r) * 64 + lane];
+    }
+    emit(token, head, d, x, top, sum);
+  }
+}
+
+// Joins the shares of packed_narrow_kernel: a wave per (row, head), shares in order.
+template <typename T, int D> __global__ __launch_bounds__(256) void join_kernel(PackedAttnParams p, int splits, Partials part) {
+  const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (i >= p.T * p.heads) return;
+  const long long t = i / p.heads;
+  const int lane = threadIdx.x & 63;
+  const int s = search_group<64>(p.seqs.n, t, [&](int k) { return (long long)p.seqs.q_start[k]; });
+  if (s < 0) return;
+  const int a = p.seqs.q_start[s], b = p.seqs.q_start[s + 1], len = p.seqs.kv_len[s];
+  const long long k0 = p.seqs.kv_start[s];
+  if (a < 0 || t >= b || b > p.T || len < 0 || k0 < 0 || k0 > p.kv_rows - len) return;
+  const long long step = p.T * p.heads;
+  float top = kLowest;
+  for (int k = 0; k < splits; ++k) top = fmaxf(top, part.ml[k * step + i].x);
+  float sum = 0.f, x[(D + 63) / 64] = {};
+  for (int k = 0; k < splits; ++k) {
+    const float2 ml = part.ml[k * step + i];
+    if (ml.y == 0.f) continue;  // no key was seen
+    const float f = fast_exp2(ml.x - top);
+    sum += f * ml.y;
+#pragma unroll
+    for (int e = 0; e < (D + 63) / 64; ++e)
+      if (e * 64 + lane < D) x[e] += f * part.o[(k * step + i) * D + e * 64 + lane];
+  }
+  const float inv = sum != 0.f ? 1.f / sum : 0.f;
+  T* o = static_cast<T*>(p.o) + t * p.ldo + (i - t * p.heads) * D;
+#pragma unroll
+  for (int e = 0; e < (D + 63) / 64; ++e)
+    if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(x[e] * inv);
+}
+
+template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int splits, hipStream_t s) {
+  constexpr int NW = D * sizeof(T) > 256 ? 2 : 4, R = D * sizeof(T) <= 128 ? 4 : 2;
+  const int group = p.heads / p.kv_heads;
+  const long long slots = p.T * group / 32 + p.seqs.n;
+  DN_CHECK(slots * (64 * NW) < (1ll << 31), "dn_op_attention_packed: too many rows for one launch");
+  Partials part;
+  part.o = static_cast<float*>(p.ws);
+  part.ml = reinterpret_cast<float2*>(part.o + (long long)splits * p.T * p.heads * D);
+  hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R>), dim3((unsigned)slots, p.kv_heads, splits), dim3(64 * NW), 0, s, p, group, splits, part);
+  DN_HIP(hipGetLastError());
+  if (splits > 1) {
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)((p.T * p.heads + 3) / 4)), dim3(256), 0, s, p, splits, part);
+    DN_HIP(hipGetLastError());
   }
 }
 
@@ -336,14 +993,49 @@ template <typename T, int D, int NW> void launch(const PackedAttnParams& p, hipS
 
 bool attention_packed_dim(int D) { return D == 32 || D == 64 || D == 96 || D == 128; }
 
-size_t attention_packed_bytes(int, long long, int, int, int, int, int) { return 0; }
+namespace {
+
+constexpr int kCus = 256;  // (of the one GPU this is built for: sizes do not depend on the device at hand)
+
+// How a call is run: `narrow` and in how many shares of the keys, or whole tiles of rows.
+struct Plan {
+  bool narrow = false;
+  int splits = 1;
+};
+Plan plan(long long T, int heads, int kv_heads, int n, int max_kv) {
+  const long long group = heads / kv_heads, rows = T * group;
+  Plan r;
+  r.narrow = rows <= 32ll * n;
+  if (r.narrow) {
+    const long long units = (rows / 32 + n) * kv_heads;
+    r.splits = (int)std::max(1ll, std::min({(8ll * kCus + units - 1) / units, (max_kv + 255ll) / 256, 64ll}));
+  }
+  return r;
+}
+
+template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) {
+  const Plan r = plan(p.T, p.heads, p.kv_heads, p.seqs.n, p.max_kv);
+  if (r.narrow) return launch_narrow<T, D>(p, r.splits, s);
+  if constexpr (sizeof(T) == 2 && (D == 64 || D == 128)) {
+    return launch_pipe<D, 64, 8, 4, 2>(p, s);
+  } else {
+    return launch<T, D, 4>(p, s);
+  }
+}
+
+}  // namespace
+
+size_t attention_packed_bytes(int, long long T, int heads, int kv_heads, int D, int n, int max_kv) {
+  const Plan r = plan(T, heads, kv_heads, n, max_kv);
+  return r.splits > 1 ? (size_t)r.splits * T * heads * (D + 2) * sizeof(float) : 0;
+}
 
 template <typename T> void attention_packed(const PackedAttnParams& p, int D, hipStream_t s) {
   switch (D) {
-    case 32: return launch<T, 32, 4>(p, s);
-    case 64: return launch<T, 64, 4>(p, s);
-    case 96: return launch<T, 96, 4>(p, s);
-    default: return launch<T, 128, 4>(p, s);
+    case 32: return run<T, 32>(p, s);
+    case 64: return run<T, 64>(p, s);
+    case 96: return run<T, 96>(p, s);
+    default: return run<T, 128>(p, s);
   }
 }
 
