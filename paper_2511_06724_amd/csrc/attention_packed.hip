@@ -730,10 +730,12 @@ template <int D, int KT, int NW, int R, int WPE> void launch_pipe(const PackedAt
 // ---------------------------------------------------------------------------
 // Few rows per sequence (single tokens, short drafts) over many keys: bound by reading K and V once.
 //
-// A workgroup has 32 rows of a unit and one of `splits` shares of its key range. Each of its NW waves takes every
-// NW-th block of 32 keys, loaded global -> LDS into a ring of its own, so nothing waits for another wave
-// until the end, where the waves' (m, l, O) meet in LDS in wave order. With several shares the partial results go to the
-// workspace and a second kernel joins them in order: results do not depend on timing.
+// Work units are 32 rows of one (sequence, key head), each as many blocks of 32 keys long as its sequence. `shares`
+// workgroups divide all blocks of the call evenly, whatever the lengths: workgroup w takes blocks [w B / shares,
+// (w + 1) B / shares) of their concatenation, found from the lengths on the device. Within a unit each of its NW
+// waves takes every NW-th block, loaded global -> LDS into a ring of its own, so nothing waits for another wave until
+// the unit's end, where the waves' (m, l, O) meet in LDS in wave order. A unit that one workgroup has to itself is stored;
+// one that is divided goes to the workspace in parts, which a second kernel joins in order: results do not depend on timing.
 template <typename T, int D> struct Block {
   static constexpr int RB = D * (int)sizeof(T), CH = RB / 16;  // bytes and 16-byte pieces per row
   static constexpr int BYTES = 32 * RB;                        // of K, and of V
@@ -742,13 +744,64 @@ template <typename T, int D> struct Block {
   __device__ static __forceinline__ int v_piece(int row, int c) { return c ^ ((row & VX) << 1); }
 };
 
+// The workspace of divided units. A workgroup has at most two: one it comes into (part 0), one it leaves (part 1).
 struct Partials {
-  float* o = nullptr;    // [splits][T][heads][D]
-  float2* ml = nullptr;  // [splits][T][heads] (m, l)
+  long long* blocks = nullptr;  // [1] blocks of the call
+  long long* start = nullptr;   // [kv_heads][slots] first block of each unit
+  float2* ml = nullptr;         // [shares][2][32] (m, l)
+  float* o = nullptr;           // [shares][2][32][D]
 };
 
-template <typename T, int D, int NW, int R>
-__global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams p, int group, int splits, Partials part) {
+__device__ __forceinline__ int key_blocks(int len) { return max(1, (len + 31) / 32); }  // (one that stores zeros, without keys)
+
+// Sequences in order, 64 at a time in the lanes of a wave: blocks of the units (for one key head) before and in each.
+struct Walk {
+  int first = 0;             // sequence of lane 0
+  long long base = 0;        // blocks before it
+  long long incl = 0, cost = 0;
+  __device__ __forceinline__ void load(const PackedAttnParams& p, int group) {
+    const int i = first + (threadIdx.x & 63);
+    cost = 0;
+    if (i < p.seqs.n) {
+      const int a = p.seqs.q_start[i], b = p.seqs.q_start[i + 1], len = p.seqs.kv_len[i];
+      const long long k0 = p.seqs.kv_start[i];
+      if (a >= 0 && b > a && b <= p.T && len >= 0 && k0 >= 0 && k0 <= p.kv_rows - len)
+        cost = ((long long)(b - a) * group + 31) / 32 * key_blocks(len);
+    }
+    incl = cost;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const long long x = __shfl_up(incl, d, 64);
+      if ((int)(threadIdx.x & 63) >= d) incl += x;
+    }
+  }
+  __device__ __forceinline__ long long last() const { return base + __shfl(incl, 63, 64); }
+  __device__ __forceinline__ void next(const PackedAttnParams& p, int group) {
+    base = last();
+    first += 64;
+    load(p, group);
+  }
+  __device__ __forceinline__ void restart(const PackedAttnParams& p, int group) {
+    if (first == 0) return;
+    first = 0;
+    base = 0;
+    load(p, group);
+  }
+  // sequence and first block of the one that block y belongs to; y < all blocks, not before `base`
+  __device__ __forceinline__ int find(const PackedAttnParams& p, int group, long long y, long long& at) {
+    while (y >= last()) next(p, group);
+    const int i = __ffsll((unsigned long long)__ballot(base + incl > y)) - 1;
+    at = base + __shfl(incl - cost, i, 64);
+    return first + i;
+  }
+};
+
+__device__ __forceinline__ long long uniform(long long x) {
+  return (long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+template <typename T, int D, int NW, int R, bool DIVIDED>
+__global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams p, int group, int slots, int shares, Partials part) {
   using MM = Mma<T>;
   using BL = Block<T, D>;
   constexpr int NV = BL::CH / 2;             // 16-byte operands of a K or Q row per lane
@@ -757,32 +810,73 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
   constexpr int RING = NW * R * 2 * BL::BYTES, CARE = 2 * kKT * (D + 16 / (int)sizeof(T)) * (int)sizeof(T), JOIN = NW * (DB * 16 * 64 + 64) * 4;
   constexpr int LDS = RING > CARE ? (RING > JOIN ? RING : JOIN) : (CARE > JOIN ? CARE : JOIN);
   __shared__ __align__(16) unsigned char lds[LDS];
-
-  Unit u;
-  if (!find_unit<32>(p, group, blockIdx.x, u)) return;
-  u.rows = min(u.rows, u.row0 + 32);
-  const int kvh = blockIdx.y, split = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, r32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  Walk walk;
+  long long per_head = 1, x0 = 0, x1 = 1;  // blocks of one key head; the workgroup's
+  if constexpr (DIVIDED) {
+    walk.load(p, group);
+    per_head = walk.last();
+    while (walk.first + 64 < p.seqs.n) {
+      walk.next(p, group);
+      per_head = walk.last();
+    }
+    walk.restart(p, group);
+    per_head = uniform(per_head);
+    const long long blocks = per_head * p.kv_heads;
+    if (blockIdx.x == 0 && tid == 0) *part.blocks = blocks;
+    const long long g = min((long long)shares, blocks);  // (with fewer blocks than workgroups the last have none)
+    if (blockIdx.x >= g) return;
+    x0 = blocks * blockIdx.x / g;
+    x1 = blocks * (blockIdx.x + 1) / g;
+  }
+  while (x0 < x1) {
+  Unit u;
+  int kvh = blockIdx.y, b0 = 0, b1;
+  bool whole = true;
+  long long unit_part = 0;
+  if constexpr (DIVIDED) {
+    kvh = (int)(x0 / per_head);
+    const long long y = x0 - kvh * per_head;
+    if (y < walk.base) walk.restart(p, group);
+    long long seq_at;
+    const int seq = __builtin_amdgcn_readfirstlane(walk.find(p, group, y, seq_at));
+    const int qa = __builtin_amdgcn_readfirstlane(p.seqs.q_start[seq]);
+    u.q0 = qa;
+    u.len_q = __builtin_amdgcn_readfirstlane(p.seqs.q_start[seq + 1]) - qa;
+    u.len_k = __builtin_amdgcn_readfirstlane(p.seqs.kv_len[seq]);
+    u.k0 = uniform(p.seqs.kv_start[seq]);
+    const int nb = key_blocks(u.len_k);
+    const long long in = uniform(y - seq_at);
+    const int tile = (int)(in / nb);
+    b0 = (int)(in - (long long)tile * nb);
+    b1 = b0 + (int)min((long long)(nb - b0), x1 - x0);
+    u.row0 = tile * 32;
+    u.rows = (int)min((long long)u.len_q * group, u.row0 + 32ll);
+    whole = b0 == 0 && b1 == nb;
+    unit_part = 2ll * blockIdx.x + (b0 == 0 ? 1 : 0);
+    if (b0 == 0 && tid == 0) part.start[(long long)kvh * slots + (long long)qa * group / 32 + seq + tile] = x0;
+    x0 += b1 - b0;
+  } else {
+    if (!find_unit<32>(p, group, blockIdx.x, u)) return;
+    u.rows = min(u.rows, u.row0 + 32);
+    b1 = key_blocks(u.len_k);
+    ++x0;
+  }
+
   const int row = min(u.row0 + r32, u.rows - 1), token = row / group, head = kvh * group + row - token * group;
   const int lim = limit(p, u, token);
   const int range = __builtin_amdgcn_readfirstlane(limit(p, u, (u.rows - 1) / group));
   const int lo = __builtin_amdgcn_readfirstlane(limit(p, u, u.row0 / group));
-  const long long blocks = (range + 31) / 32;
-  const int b0 = (int)(blocks * split / splits), b1 = (int)(blocks * (split + 1) / splits);
   const int end = min(range, b1 * 32);
-  auto at = [&](int tok, int h) { return ((long long)split * p.T + u.q0 + tok) * p.heads + h; };
   auto emit = [&](int tok, int h, int d, const f32x16& x, float m, float sum) {
-    if (splits == 1) return store_block<T>(row_out<T>(p, u, tok, h, D) + 32 * d, x, sum);
-    float* o = part.o + at(tok, h) * D + 32 * d + 4 * half;
+    if (whole) return store_block<T>(row_out<T>(p, u, tok, h, D) + 32 * d, x, sum);
+    float* o = part.o + (unit_part * 32 + r32) * D + 32 * d + 4 * half;
 #pragma unroll
     for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(o + 8 * g) = f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
-    if (d == 0 && half == 0) part.ml[at(tok, h)] = make_float2(m, sum);
+    if (d == 0 && half == 0) part.ml[unit_part * 32 + r32] = make_float2(m, sum);
   };
-  if (b0 >= b1 && splits > 1) {  // no keys: nothing to join
-    if (wave == 0 && half == 0 && u.row0 + r32 < u.rows) part.ml[at(token, head)] = make_float2(kLowest, 0.f);
-    return;
-  }
 
   const T* qp = static_cast<const T*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D + half * (16 / sizeof(T));
   uint4 qv[NV];
@@ -814,7 +908,8 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m = kLowest, l = 0.f;
-  const int mine = b1 - b0 > wave ? (b1 - b0 - wave + NW - 1) / NW : 0;  // blocks of the wave
+  const int nk = (end + 31) / 32 - b0;                                   // blocks with keys (some rows see)
+  const int mine = nk > wave ? (nk - wave + NW - 1) / NW : 0;            // of the wave
   if (mine > 0) {
 #pragma unroll
     for (int i = 0; i < R - 1; ++i) issue(b0 + wave + min(i, mine - 1) * NW, i);
@@ -896,7 +991,9 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
   l += __shfl_xor(l, 32, 64);
   if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds))) {
     __syncthreads();
-    return careful_rows<T, D, NW>(p, u, group, kvh, reinterpret_cast<T*>(lds), b0 * 32, end, emit);
+    careful_rows<T, D, NW>(p, u, group, kvh, reinterpret_cast<T*>(lds), b0 * 32, end, emit);
+    __syncthreads();
+    continue;
   }
   __syncthreads();
 
@@ -912,72 +1009,107 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
     sm[NW * 32 + wave * 32 + r32] = l;
   }
   __syncthreads();
-  if (u.row0 + r32 >= u.rows) return;
-  float top = sm[r32], sum = 0.f, f[NW];
+  if (u.row0 + r32 < u.rows) {
+    float top = sm[r32], sum = 0.f, f[NW];
 #pragma unroll
-  for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w * 32 + r32]);
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w * 32 + r32]);
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    f[w] = fast_exp2(sm[w * 32 + r32] - top);
-    sum += f[w] * sm[NW * 32 + w * 32 + r32];
-  }
-  for (int d = wave; d < DB; d += NW) {
-    f32x16 x;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r] = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) x[r] += f[w] * so[((w * DB + d) * 16 + r) * 64 + lane];
+    for (int w = 0; w < NW; ++w) {
+      f[w] = fast_exp2(sm[w * 32 + r32] - top);
+      sum += f[w] * sm[NW * 32 + w * 32 + r32];
     }
-    emit(token, head, d, x, top, sum);
+    for (int d = wave; d < DB; d += NW) {
+      f32x16 x;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) x[r] += f[w] * so[((w * DB + d) * 16 + r) * 64 + lane];
+      }
+      emit(token, head, d, x, top, sum);
+    }
+  }
+  __syncthreads();
   }
 }
 
-// Joins the shares of packed_narrow_kernel: a wave per (row, head), shares in order.
-template <typename T, int D> __global__ __launch_bounds__(256) void join_kernel(PackedAttnParams p, int splits, Partials part) {
+// Joins the parts of divided units: a wave per (row, head), parts in order, a lane holding the statistics of one.
+template <typename T, int D> __global__ __launch_bounds__(256) void join_kernel(PackedAttnParams p, int group, int slots, int shares, Partials part) {
+  constexpr int E = (D + 63) / 64;
   const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= p.T * p.heads) return;
   const long long t = i / p.heads;
-  const int lane = threadIdx.x & 63;
+  const int head = (int)(i - t * p.heads), kvh = head / group, lane = threadIdx.x & 63;
   const int s = search_group<64>(p.seqs.n, t, [&](int k) { return (long long)p.seqs.q_start[k]; });
   if (s < 0) return;
   const int a = p.seqs.q_start[s], b = p.seqs.q_start[s + 1], len = p.seqs.kv_len[s];
   const long long k0 = p.seqs.kv_start[s];
   if (a < 0 || t >= b || b > p.T || len < 0 || k0 < 0 || k0 > p.kv_rows - len) return;
-  const long long step = p.T * p.heads;
+  const int row = (int)(t - a) * group + head - kvh * group;
+  const long long blocks = *part.blocks, x = part.start[(long long)kvh * slots + (long long)a * group / 32 + s + row / 32];
+  // workgroup of a block: the last w with w blocks / g <= it
+  const long long g = min((long long)shares, blocks);
+  const long long w0 = ((x + 1) * g - 1) / blocks, w1 = ((x + key_blocks(len)) * g - 1) / blocks;
+  if (w0 == w1) return;  // stored whole
+  auto at = [&](long long w) { return (2 * w + (w == w0 ? 1 : 0)) * 32 + (row & 31); };
   float top = kLowest;
-  for (int k = 0; k < splits; ++k) top = fmaxf(top, part.ml[k * step + i].x);
-  float sum = 0.f, x[(D + 63) / 64] = {};
-  for (int k = 0; k < splits; ++k) {
-    const float2 ml = part.ml[k * step + i];
-    if (ml.y == 0.f) continue;  // no key was seen
-    const float f = fast_exp2(ml.x - top);
-    sum += f * ml.y;
+  for (long long w = w0 + lane; w <= w1; w += 64) top = fmaxf(top, part.ml[at(w)].x);
+  top = wave_max(top);
+  float sum = 0.f, v[E] = {};
+  for (long long c = w0; c <= w1; c += 64) {
+    const float2 mine = c + lane <= w1 ? part.ml[at(c + lane)] : make_float2(kLowest, 0.f);
+    const float f = mine.y == 0.f ? 0.f : fast_exp2(mine.x - top), fl = f * mine.y;
+    const int n = (int)min(64ll, w1 - c + 1);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float fk = __shfl(f, k, 64);
+      sum += __shfl(fl, k, 64);
+      const float* o = part.o + at(c + k) * D;
 #pragma unroll
-    for (int e = 0; e < (D + 63) / 64; ++e)
-      if (e * 64 + lane < D) x[e] += f * part.o[(k * step + i) * D + e * 64 + lane];
+      for (int e = 0; e < E; ++e)
+        if (e * 64 + lane < D) v[e] += fk * o[e * 64 + lane];
+    }
   }
   const float inv = sum != 0.f ? 1.f / sum : 0.f;
-  T* o = static_cast<T*>(p.o) + t * p.ldo + (i - t * p.heads) * D;
+  T* o = static_cast<T*>(p.o) + t * p.ldo + (long long)head * D;
 #pragma unroll
-  for (int e = 0; e < (D + 63) / 64; ++e)
-    if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(x[e] * inv);
+  for (int e = 0; e < E; ++e)
+    if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(v[e] * inv);
 }
 
-template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int splits, hipStream_t s) {
-  constexpr int NW = D * sizeof(T) > 256 ? 2 : 4, R = D * sizeof(T) <= 128 ? 4 : 2;
+// Workspace layout and size (0 where every unit has a workgroup to itself).
+size_t partials(void* ws, int D, int kv_heads, long long slots, int shares, Partials& r) {
+  unsigned char* b = static_cast<unsigned char*>(ws);
+  size_t n = 0;
+  auto take = [&](size_t bytes) {
+    unsigned char* x = b ? b + n : nullptr;
+    n += (bytes + 255) / 256 * 256;
+    return x;
+  };
+  r.blocks = reinterpret_cast<long long*>(take(sizeof(long long)));
+  r.start = reinterpret_cast<long long*>(take(sizeof(long long) * kv_heads * slots));
+  r.ml = reinterpret_cast<float2*>(take(sizeof(float2) * 64 * shares));
+  r.o = reinterpret_cast<float*>(take(sizeof(float) * 64 * shares * D));
+  return n;
+}
+
+#ifndef NWX
+#define NWX 4
+#endif
+template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int shares, hipStream_t s) {
+  constexpr int NW = D * sizeof(T) > 256 ? 2 : NWX, R = D * sizeof(T) <= 128 ? 4 : 2;
   const int group = p.heads / p.kv_heads;
   const long long slots = p.T * group / 32 + p.seqs.n;
-  DN_CHECK(slots * (64 * NW) < (1ll << 31), "dn_op_attention_packed: too many rows for one launch");
   Partials part;
-  part.o = static_cast<float*>(p.ws);
-  part.ml = reinterpret_cast<float2*>(part.o + (long long)splits * p.T * p.heads * D);
-  hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R>), dim3((unsigned)slots, p.kv_heads, splits), dim3(64 * NW), 0, s, p, group, splits, part);
-  DN_HIP(hipGetLastError());
-  if (splits > 1) {
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)((p.T * p.heads + 3) / 4)), dim3(256), 0, s, p, splits, part);
+  if (shares) {
+    partials(p.ws, D, p.kv_heads, slots, shares, part);
+    hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R, true>), dim3(shares), dim3(64 * NW), 0, s, p, group, (int)slots, shares, part);
     DN_HIP(hipGetLastError());
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)((p.T * p.heads + 3) / 4)), dim3(256), 0, s, p, group, (int)slots, shares, part);
+  } else {
+    hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R, false>), dim3((unsigned)slots, p.kv_heads), dim3(64 * NW), 0, s, p, group, (int)slots, 0, part);
   }
+  DN_HIP(hipGetLastError());
 }
 
 template <typename T, int D, int NW> void launch(const PackedAttnParams& p, hipStream_t s) {
@@ -997,25 +1129,28 @@ namespace {
 
 constexpr int kCus = 256;  // (of the one GPU this is built for: sizes do not depend on the device at hand)
 
-// How a call is run: `narrow` and in how many shares of the keys, or whole tiles of rows.
+#ifndef SHX
+#define SHX 256
+#endif
+// How a call is run: `narrow` (32 rows a unit; `shares` workgroups over all key blocks, 0: one per unit), or whole tiles.
 struct Plan {
   bool narrow = false;
-  int splits = 1;
+  int shares = 0;
 };
 Plan plan(long long T, int heads, int kv_heads, int n, int max_kv) {
   const long long group = heads / kv_heads, rows = T * group;
   Plan r;
-  r.narrow = rows <= 32ll * n;
-  if (r.narrow) {
-    const long long units = (rows / 32 + n) * kv_heads;
-    r.splits = (int)std::max(1ll, std::min({(8ll * kCus + units - 1) / units, (max_kv + 255ll) / 256, 64ll}));
+  r.narrow = rows <= 32ll * n && T * heads < (1 << 26) - 4;
+  if (r.narrow && max_kv > 256) {
+    const long long units = (rows / 32 + n) * kv_heads, blocks = units * ((max_kv + 31ll) / 32);
+    r.shares = (int)std::min<long long>(SHX, (blocks + 7) / 8);
   }
   return r;
 }
 
 template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) {
   const Plan r = plan(p.T, p.heads, p.kv_heads, p.seqs.n, p.max_kv);
-  if (r.narrow) return launch_narrow<T, D>(p, r.splits, s);
+  if (r.narrow) return launch_narrow<T, D>(p, r.shares, s);
   if constexpr (sizeof(T) == 2 && (D == 64 || D == 128)) {
     return launch_pipe<D, 64, 8, 4, 2>(p, s);
   } else {
@@ -1025,9 +1160,10 @@ template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) 
 
 }  // namespace
 
-size_t attention_packed_bytes(int, long long T, int heads, int kv_heads, int D, int n, int max_kv) {
+size_t attention_packed_bytes(long long T, int heads, int kv_heads, int D, int n, int max_kv) {
   const Plan r = plan(T, heads, kv_heads, n, max_kv);
-  return r.splits > 1 ? (size_t)r.splits * T * heads * (D + 2) * sizeof(float) : 0;
+  Partials part;
+  return r.shares ? partials(nullptr, D, kv_heads, T * (heads / kv_heads) / 32 + n, r.shares, part) : 0;
 }
 
 template <typename T> void attention_packed(const PackedAttnParams& p, int D, hipStream_t s) {
