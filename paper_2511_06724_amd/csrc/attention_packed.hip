@@ -28,6 +28,7 @@
 // out of masked tiles, adding them back where they are seen (one tile a work unit at most, plus the
 // border of the range).
 #include <algorithm>
+#include <cmath>
 
 #include "lane_swap.h"
 #include "packed.h"
@@ -728,6 +729,16 @@ template <int D, int KT, int NW, int R, int WPE> void launch_pipe(const PackedAt
 }
 
 // ---------------------------------------------------------------------------
+// 16 bytes per lane global -> LDS as dma16_base, for data that is read once: past the caches the same reads reach 6.5 TB/s,
+// through them 5.6 (1.07 GB, rows of 256 bytes 2 KB apart).
+__device__ __forceinline__ void dma16_stream(const char* base, unsigned off, lds_void* lds) {
+  const unsigned a = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(reinterpret_cast<__UINTPTR_TYPE__>(lds)));
+  const unsigned long long b = reinterpret_cast<__UINTPTR_TYPE__>(base);
+  const unsigned long long u = static_cast<unsigned long long>(__builtin_amdgcn_readfirstlane(static_cast<unsigned>(b >> 32))) << 32 |
+                               static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<unsigned>(b)));
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(u), "s"(a) : "memory", "m0");
+}
+
 // Few rows per sequence (single tokens, short drafts) over many keys: bound by reading K and V once.
 //
 // Work units are 32 rows of one (sequence, key head), each as many blocks of 32 keys long as its sequence. `shares`
@@ -745,28 +756,39 @@ template <typename T, int D> struct Block {
 };
 
 // The workspace of divided units. A workgroup has at most two: one it comes into (part 0), one it leaves (part 1).
+// A divided unit belongs to the workgroup that begins it: `rows` (0: the workgroup leaves none) from row0 of the
+// sequence at packed row q0, workgroups up to `last`.
+struct DividedUnit {
+  int rows, row0, kvh, last;
+  long long q0;
+};
 struct Partials {
-  long long* blocks = nullptr;  // [1] blocks of the call
-  long long* start = nullptr;   // [kv_heads][slots] first block of each unit
+  DividedUnit* unit = nullptr;  // [shares]
   float2* ml = nullptr;         // [shares][2][32] (m, l)
   float* o = nullptr;           // [shares][2][32][D]
 };
 
 __device__ __forceinline__ int key_blocks(int len) { return max(1, (len + 31) / 32); }  // (one that stores zeros, without keys)
 
+__device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ long long from_lane(long long x, int lane) {
+  return (long long)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
+}
+
 // Sequences in order, 64 at a time in the lanes of a wave: blocks of the units (for one key head) before and in each.
 struct Walk {
   int first = 0;             // sequence of lane 0
   long long base = 0;        // blocks before it
-  long long incl = 0, cost = 0;
+  long long incl = 0, cost = 0, k0 = 0;
+  int qa = 0, qb = 0, len = 0;
   __device__ __forceinline__ void load(const PackedAttnParams& p, int group) {
     const int i = first + (threadIdx.x & 63);
     cost = 0;
     if (i < p.seqs.n) {
-      const int a = p.seqs.q_start[i], b = p.seqs.q_start[i + 1], len = p.seqs.kv_len[i];
-      const long long k0 = p.seqs.kv_start[i];
-      if (a >= 0 && b > a && b <= p.T && len >= 0 && k0 >= 0 && k0 <= p.kv_rows - len)
-        cost = ((long long)(b - a) * group + 31) / 32 * key_blocks(len);
+      qa = p.seqs.q_start[i], qb = p.seqs.q_start[i + 1], len = p.seqs.kv_len[i];
+      k0 = p.seqs.kv_start[i];
+      if (qa >= 0 && qb > qa && qb <= p.T && len >= 0 && k0 >= 0 && k0 <= p.kv_rows - len)
+        cost = ((long long)(qb - qa) * group + 31) / 32 * key_blocks(len);
     }
     incl = cost;
 #pragma unroll
@@ -775,7 +797,7 @@ struct Walk {
       if ((int)(threadIdx.x & 63) >= d) incl += x;
     }
   }
-  __device__ __forceinline__ long long last() const { return base + __shfl(incl, 63, 64); }
+  __device__ __forceinline__ long long last() const { return base + from_lane(incl, 63); }
   __device__ __forceinline__ void next(const PackedAttnParams& p, int group) {
     base = last();
     first += 64;
@@ -787,21 +809,15 @@ struct Walk {
     base = 0;
     load(p, group);
   }
-  // sequence and first block of the one that block y belongs to; y < all blocks, not before `base`
-  __device__ __forceinline__ int find(const PackedAttnParams& p, int group, long long y, long long& at) {
+  // lane of the sequence that block y belongs to; y < all blocks, not before `base`
+  __device__ __forceinline__ int find(const PackedAttnParams& p, int group, long long y) {
     while (y >= last()) next(p, group);
-    const int i = __ffsll((unsigned long long)__ballot(base + incl > y)) - 1;
-    at = base + __shfl(incl - cost, i, 64);
-    return first + i;
+    return __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(base + incl > y)) - 1);
   }
 };
 
-__device__ __forceinline__ long long uniform(long long x) {
-  return (long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
-}
-
 template <typename T, int D, int NW, int R, bool DIVIDED>
-__global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams p, int group, int slots, int shares, Partials part) {
+__global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams p, int group, int shares, Partials part) {
   using MM = Mma<T>;
   using BL = Block<T, D>;
   constexpr int NV = BL::CH / 2;             // 16-byte operands of a K or Q row per lane
@@ -823,10 +839,9 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
       per_head = walk.last();
     }
     walk.restart(p, group);
-    per_head = uniform(per_head);
     const long long blocks = per_head * p.kv_heads;
-    if (blockIdx.x == 0 && tid == 0) *part.blocks = blocks;
     const long long g = min((long long)shares, blocks);  // (with fewer blocks than workgroups the last have none)
+    if (tid == 0) part.unit[blockIdx.x].rows = 0;
     if (blockIdx.x >= g) return;
     x0 = blocks * blockIdx.x / g;
     x1 = blocks * (blockIdx.x + 1) / g;
@@ -840,15 +855,14 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
     kvh = (int)(x0 / per_head);
     const long long y = x0 - kvh * per_head;
     if (y < walk.base) walk.restart(p, group);
-    long long seq_at;
-    const int seq = __builtin_amdgcn_readfirstlane(walk.find(p, group, y, seq_at));
-    const int qa = __builtin_amdgcn_readfirstlane(p.seqs.q_start[seq]);
+    const int i = walk.find(p, group, y);
+    const int qa = from_lane(walk.qa, i);
     u.q0 = qa;
-    u.len_q = __builtin_amdgcn_readfirstlane(p.seqs.q_start[seq + 1]) - qa;
-    u.len_k = __builtin_amdgcn_readfirstlane(p.seqs.kv_len[seq]);
-    u.k0 = uniform(p.seqs.kv_start[seq]);
+    u.len_q = from_lane(walk.qb, i) - qa;
+    u.len_k = from_lane(walk.len, i);
+    u.k0 = from_lane(walk.k0, i);
     const int nb = key_blocks(u.len_k);
-    const long long in = uniform(y - seq_at);
+    const long long in = y - (walk.base + from_lane(walk.incl - walk.cost, i));
     const int tile = (int)(in / nb);
     b0 = (int)(in - (long long)tile * nb);
     b1 = b0 + (int)min((long long)(nb - b0), x1 - x0);
@@ -856,7 +870,11 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
     u.rows = (int)min((long long)u.len_q * group, u.row0 + 32ll);
     whole = b0 == 0 && b1 == nb;
     unit_part = 2ll * blockIdx.x + (b0 == 0 ? 1 : 0);
-    if (b0 == 0 && tid == 0) part.start[(long long)kvh * slots + (long long)qa * group / 32 + seq + tile] = x0;
+    if (b0 == 0 && !whole && tid == 0) {
+      // the last workgroup w with w blocks / g <= the unit's last block
+      const long long blocks = per_head * p.kv_heads, g = min((long long)shares, blocks);
+      part.unit[blockIdx.x] = DividedUnit{u.rows - u.row0, u.row0, kvh, (int)(((x0 + nb) * g - 1) / blocks), u.q0};
+    }
     x0 += b1 - b0;
   } else {
     if (!find_unit<32>(p, group, blockIdx.x, u)) return;
@@ -885,21 +903,28 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
   const char* kbase = reinterpret_cast<const char*>(static_cast<const T*>(p.k) + u.k0 * p.ldk + (long long)kvh * D);
   const char* vbase = reinterpret_cast<const char*>(static_cast<const T*>(p.v) + u.k0 * p.ldv + (long long)kvh * D);
   unsigned char* ring = lds + wave * R * 2 * BL::BYTES;
-  auto issue = [&](int b, int slot) {  // block b, or the range's last key where it has none
+  unsigned koff[LW], voff[LW];
+  auto set_offsets = [&](int keys) {  // of a block that has `keys` keys: the rows past them read the last one
+#pragma unroll
+    for (int j = 0; j < LW; ++j) {
+      const int w = j * 64 + lane, r = w / BL::CH, ch = w - r * BL::CH;
+      const unsigned key = (unsigned)min(r, keys - 1) * (unsigned)sizeof(T);
+      koff[j] = key * (unsigned)p.ldk + 16u * BL::k_piece(r, ch);
+      voff[j] = key * (unsigned)p.ldv + 16u * BL::v_piece(r, ch);
+    }
+  };
+  set_offsets(32);
+  auto issue = [&](int b, int slot) {
     const char* kb = kbase + (long long)b * 32 * p.ldk * (int)sizeof(T);
     const char* vb = vbase + (long long)b * 32 * p.ldv * (int)sizeof(T);
+    unsigned char* to = ring + slot * 2 * BL::BYTES;
+    const bool partial = (b + 1) * 32 > end;
+    if (partial) set_offsets(end - b * 32);
 #pragma unroll
-    for (int j = 0; j < LW; ++j) {
-      const int w = j * 64 + lane, r = w / BL::CH, ch = w - r * BL::CH;
-      const unsigned key = (unsigned)(min(b * 32 + r, end - 1) - b * 32);
-      dma16_base(kb, key * (unsigned)p.ldk * (unsigned)sizeof(T) + 16u * BL::k_piece(r, ch), (lds_void*)(ring + slot * 2 * BL::BYTES + j * 1024));
-    }
+    for (int j = 0; j < LW; ++j) dma16_stream(kb, koff[j], (lds_void*)(to + j * 1024));
 #pragma unroll
-    for (int j = 0; j < LW; ++j) {
-      const int w = j * 64 + lane, r = w / BL::CH, ch = w - r * BL::CH;
-      const unsigned key = (unsigned)(min(b * 32 + r, end - 1) - b * 32);
-      dma16_base(vb, key * (unsigned)p.ldv * (unsigned)sizeof(T) + 16u * BL::v_piece(r, ch), (lds_void*)(ring + slot * 2 * BL::BYTES + BL::BYTES + j * 1024));
-    }
+    for (int j = 0; j < LW; ++j) dma16_stream(vb, voff[j], (lds_void*)(to + BL::BYTES + j * 1024));
+    if (partial) set_offsets(32);
   };
 
   f32x16 o[DB];
@@ -1033,52 +1058,69 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
   }
 }
 
-// Joins the parts of divided units: a wave per (row, head), parts in order, a lane holding the statistics of one.
-template <typename T, int D> __global__ __launch_bounds__(256) void join_kernel(PackedAttnParams p, int group, int slots, int shares, Partials part) {
+// Joins the parts of a divided unit: a workgroup per row, whose wave w takes parts w, w + kJoin, ..; then the waves' sums
+// in order. A lane holds the statistics of one part and D / 64 of the row's values.
+constexpr int kJoin = 8;
+template <typename T, int D> __global__ __launch_bounds__(64 * kJoin) void join_kernel(PackedAttnParams p, int group, Partials part) {
   constexpr int E = (D + 63) / 64;
-  const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= p.T * p.heads) return;
-  const long long t = i / p.heads;
-  const int head = (int)(i - t * p.heads), kvh = head / group, lane = threadIdx.x & 63;
-  const int s = search_group<64>(p.seqs.n, t, [&](int k) { return (long long)p.seqs.q_start[k]; });
-  if (s < 0) return;
-  const int a = p.seqs.q_start[s], b = p.seqs.q_start[s + 1], len = p.seqs.kv_len[s];
-  const long long k0 = p.seqs.kv_start[s];
-  if (a < 0 || t >= b || b > p.T || len < 0 || k0 < 0 || k0 > p.kv_rows - len) return;
-  const int row = (int)(t - a) * group + head - kvh * group;
-  const long long blocks = *part.blocks, x = part.start[(long long)kvh * slots + (long long)a * group / 32 + s + row / 32];
-  // workgroup of a block: the last w with w blocks / g <= it
-  const long long g = min((long long)shares, blocks);
-  const long long w0 = ((x + 1) * g - 1) / blocks, w1 = ((x + key_blocks(len)) * g - 1) / blocks;
-  if (w0 == w1) return;  // stored whole
-  auto at = [&](long long w) { return (2 * w + (w == w0 ? 1 : 0)) * 32 + (row & 31); };
-  float top = kLowest;
-  for (long long w = w0 + lane; w <= w1; w += 64) top = fmaxf(top, part.ml[at(w)].x);
-  top = wave_max(top);
-  float sum = 0.f, v[E] = {};
-  for (long long c = w0; c <= w1; c += 64) {
-    const float2 mine = c + lane <= w1 ? part.ml[at(c + lane)] : make_float2(kLowest, 0.f);
-    const float f = mine.y == 0.f ? 0.f : fast_exp2(mine.x - top), fl = f * mine.y;
-    const int n = (int)min(64ll, w1 - c + 1);
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-      const float fk = __shfl(f, k, 64);
-      sum += __shfl(fl, k, 64);
-      const float* o = part.o + at(c + k) * D;
+  __shared__ float s_v[kJoin][E * 64], s_top[kJoin], s_sum[kJoin];
+  const int w0 = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const DividedUnit u = part.unit[w0];
+  const int n = u.last - w0 + 1;
+  for (int r = blockIdx.y; r < u.rows; r += gridDim.y) {
+    auto at = [&](int k) { return (2ll * (w0 + k) + (k == 0 ? 1 : 0)) * 32 + r; };
+    float sum = 0.f, v[E] = {}, top = kLowest;
+    for (int c = wave; c < n; c += 64 * kJoin) {
+      const int mine = c + lane * kJoin;
+      const float2 ml = mine < n ? part.ml[at(mine)] : make_float2(kLowest, 0.f);
+      const float up = fmaxf(top, wave_max(ml.x)), alpha = fast_exp2(top - up);
+      top = up;
+      sum *= alpha;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] *= alpha;
+      const float f = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top), fl = f * ml.y;
+      const int cnt = min(64, (n - c + kJoin - 1) / kJoin);
+#pragma unroll 8
+      for (int k = 0; k < cnt; ++k) {
+        const float fk = __shfl(f, k, 64);
+        sum += __shfl(fl, k, 64);
+        const float* o = part.o + at(c + k * kJoin) * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] += fk * o[min(e * 64 + lane, D - 1)];  // (without a branch: loads side by side)
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_v[wave][e * 64 + lane] = v[e];
+    if (lane == 0) {
+      s_top[wave] = top;
+      s_sum[wave] = sum;
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int k = 1; k < kJoin; ++k) top = fmaxf(top, s_top[k]);
+      float total = 0.f, x[E] = {};
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        const float f = fast_exp2(s_top[k] - top);
+        total += f * s_sum[k];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += f * s_v[k][e * 64 + lane];
+      }
+      const float inv = total != 0.f ? 1.f / total : 0.f;
+      const int row = u.row0 + r, token = row / group;
+      T* o = static_cast<T*>(p.o) + (u.q0 + token) * p.ldo + (long long)(u.kvh * group + row - token * group) * D;
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (e * 64 + lane < D) v[e] += fk * o[e * 64 + lane];
+        if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(x[e] * inv);
     }
   }
-  const float inv = sum != 0.f ? 1.f / sum : 0.f;
-  T* o = static_cast<T*>(p.o) + t * p.ldo + (long long)head * D;
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(v[e] * inv);
 }
 
 // Workspace layout and size (0 where every unit has a workgroup to itself).
-size_t partials(void* ws, int D, int kv_heads, long long slots, int shares, Partials& r) {
+size_t partials(void* ws, int D, int shares, Partials& r) {
   unsigned char* b = static_cast<unsigned char*>(ws);
   size_t n = 0;
   auto take = [&](size_t bytes) {
@@ -1086,28 +1128,40 @@ size_t partials(void* ws, int D, int kv_heads, long long slots, int shares, Part
     n += (bytes + 255) / 256 * 256;
     return x;
   };
-  r.blocks = reinterpret_cast<long long*>(take(sizeof(long long)));
-  r.start = reinterpret_cast<long long*>(take(sizeof(long long) * kv_heads * slots));
+  r.unit = reinterpret_cast<DividedUnit*>(take(sizeof(DividedUnit) * shares));
   r.ml = reinterpret_cast<float2*>(take(sizeof(float2) * 64 * shares));
   r.o = reinterpret_cast<float*>(take(sizeof(float) * 64 * shares * D));
   return n;
 }
 
-#ifndef NWX
-#define NWX 4
-#endif
+// Divided calls: one wave a workgroup, up to 1024 of them (four a CU, by their rings): 32 contexts up to 54 k, 32/8 heads of
+// 128: 181 us, with two waves and 512 200, with four and 256 212. Others: four waves on a unit.
+constexpr int kShares = 1024;
+
+// Of few blocks the shares are fewer: a block takes a wave about 1 us and a part takes the join about 0.04 us, and
+// one unit may have the shares of its key head to itself, so s shares of B blocks take B / s + 0.04 s / kv_heads.
+int shares_of(long long blocks, int kv_heads, long long units) {
+  const long long s = (long long)(5.0 * std::sqrt((double)blocks * kv_heads));
+  return (int)std::min({std::max(s, units), blocks, (long long)kShares});
+}
+
 template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int shares, hipStream_t s) {
-  constexpr int NW = D * sizeof(T) > 256 ? 2 : NWX, R = D * sizeof(T) <= 128 ? 4 : 2;
-  const int group = p.heads / p.kv_heads;
-  const long long slots = p.T * group / 32 + p.seqs.n;
+  constexpr int R = D * sizeof(T) <= 128 ? 4 : 2;
+  const long long group = p.heads / p.kv_heads, rows = p.T * group;
   Partials part;
   if (shares) {
-    partials(p.ws, D, p.kv_heads, slots, shares, part);
-    hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R, true>), dim3(shares), dim3(64 * NW), 0, s, p, group, (int)slots, shares, part);
+    partials(p.ws, D, shares, part);
+    // the tensors' rows bound the blocks, too
+    const long long blocks = (p.kv_rows / 32 + p.seqs.n) * p.kv_heads * ((rows + 32ll * p.seqs.n - 1) / (32ll * p.seqs.n));
+    shares = std::min(shares, shares_of(blocks, p.kv_heads, (rows / 32 + p.seqs.n) * p.kv_heads));
+    hipLaunchKernelGGL((packed_narrow_kernel<T, D, 1, R, true>), dim3(shares), dim3(64), 0, s, p, (int)group, shares, part);
     DN_HIP(hipGetLastError());
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)((p.T * p.heads + 3) / 4)), dim3(256), 0, s, p, group, (int)slots, shares, part);
+    const long long per = std::min<long long>(32, (rows + p.seqs.n - 1) / p.seqs.n);  // rows of a unit, in the mean
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3(shares, (unsigned)per), dim3(64 * kJoin), 0, s, p, (int)group, part);
   } else {
-    hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R, false>), dim3((unsigned)slots, p.kv_heads), dim3(64 * NW), 0, s, p, group, (int)slots, 0, part);
+    constexpr int NW = D * sizeof(T) > 256 ? 2 : 4;
+    const long long slots = rows / 32 + p.seqs.n;
+    hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R, false>), dim3((unsigned)slots, p.kv_heads), dim3(64 * NW), 0, s, p, (int)group, 0, part);
   }
   DN_HIP(hipGetLastError());
 }
@@ -1129,9 +1183,6 @@ namespace {
 
 constexpr int kCus = 256;  // (of the one GPU this is built for: sizes do not depend on the device at hand)
 
-#ifndef SHX
-#define SHX 256
-#endif
 // How a call is run: `narrow` (32 rows a unit; `shares` workgroups over all key blocks, 0: one per unit), or whole tiles.
 struct Plan {
   bool narrow = false;
@@ -1143,7 +1194,7 @@ Plan plan(long long T, int heads, int kv_heads, int n, int max_kv) {
   r.narrow = rows <= 32ll * n && T * heads < (1 << 26) - 4;
   if (r.narrow && max_kv > 256) {
     const long long units = (rows / 32 + n) * kv_heads, blocks = units * ((max_kv + 31ll) / 32);
-    r.shares = (int)std::min<long long>(SHX, (blocks + 7) / 8);
+    r.shares = (int)std::min<long long>(kShares, blocks);
   }
   return r;
 }
@@ -1163,7 +1214,7 @@ template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) 
 size_t attention_packed_bytes(long long T, int heads, int kv_heads, int D, int n, int max_kv) {
   const Plan r = plan(T, heads, kv_heads, n, max_kv);
   Partials part;
-  return r.shares ? partials(nullptr, D, kv_heads, T * (heads / kv_heads) / 32 + n, r.shares, part) : 0;
+  return r.shares ? partials(nullptr, D, r.shares, part) : 0;
 }
 
 template <typename T> void attention_packed(const PackedAttnParams& p, int D, hipStream_t s) {
