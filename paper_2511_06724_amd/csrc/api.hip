@@ -892,7 +892,7 @@ dn_status dn_attention_packed_bytes(int32_t dtype, int64_t T, int32_t heads, int
     check_packed_sizes("dn_attention_packed_bytes", dtype, T, heads, kv_heads, head_dim);
     DN_CHECK(n >= 1 && max_kv_len >= 1, "dn_attention_packed_bytes: bad sizes");
     *bytes = static_cast<int64_t>(
-        dn::attention_packed_bytes(T, heads, kv_heads, head_dim, n, max_kv_len));
+        dn::attention_packed_bytes(dtype == DN_BF16 ? 2 : 4, T, heads, kv_heads, head_dim, n, max_kv_len));
   });
 }
 
@@ -925,7 +925,7 @@ dn_status dn_op_attention_packed(int32_t dtype, const void* q, int64_t ldq, cons
     p.scale_log2 = scale * 1.4426950408889634f;
     p.ws = ws;
     DN_CHECK(ws ? on(ws, 16)
-                : dn::attention_packed_bytes(T, heads, kv_heads, head_dim, seqs->n, p.max_kv) == 0,
+                : dn::attention_packed_bytes(dtype == DN_BF16 ? 2 : 4, T, heads, kv_heads, head_dim, seqs->n, p.max_kv) == 0,
              "dn_op_attention_packed: the workspace of dn_attention_packed_bytes is needed, 16-byte aligned");
     dtype == DN_BF16 ? dn::attention_packed<dn::bf16>(p, head_dim, as_stream(stream))
                      : dn::attention_packed<float>(p, head_dim, as_stream(stream));

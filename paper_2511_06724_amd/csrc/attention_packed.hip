@@ -1181,38 +1181,56 @@ bool attention_packed_dim(int D) { return D == 32 || D == 64 || D == 96 || D == 
 
 namespace {
 
-constexpr int kCus = 256;  // (of the one GPU this is built for: sizes do not depend on the device at hand)
-
-// How a call is run: `narrow` (32 rows a unit; `shares` workgroups over all key blocks, 0: one per unit), or whole tiles.
+// How a call is run. A function of sizes alone (of the 256 CUs of the one GPU this is built for), so that the workspace does
+// not depend on the device at hand.
 struct Plan {
-  bool narrow = false;
-  int shares = 0;
+  bool narrow = false;  // 32 rows a unit; else whole tiles of rows
+  int shares = 0;       // most workgroups over all key blocks (0: one per unit)
+  int waves = 0;        // of 32 rows, of a tile (bf16)
 };
-Plan plan(long long T, int heads, int kv_heads, int n, int max_kv) {
-  const long long group = heads / kv_heads, rows = T * group;
+// Measured, us (heads/kv_heads x head dim):
+//  - few rows a sequence: narrow. Up to 256 keys a unit is one workgroup's (77 keys, 20/20 x 64: 6.1); longer ones are divided.
+//  - too few tiles to fill the CUs and long keys: narrow, divided (16/2 x 128, 128 tokens behind 16 k keys: 129, tiles 275;
+//    32/8 x 128, 8 x 16 behind 8 k: 126, 213; but 4 x 64 tokens: 168, tiles 143: the parts of more rows cost more).
+//  - fp32, bound by the matrix cores either way: narrow while its smaller units fill more CUs (10/2 x 64, 7 chunks behind up
+//    to 825 keys: 23.6, tiles 64.8; 12/12 x 64, 16 x 77 tokens: 21.0, 26.0; 10/10 x 64, 2 x 1024 tokens: 87, tiles 82.6).
+//  - tiles: 8 waves of 32 rows where there are tiles for every CU and the border is small beside them (20/20 x 128, two
+//    images of 4173 tokens: 357, 4 waves 402; 8 x 512 tokens: 40.0, 36.3); 2 waves for short prompts (20/20 x 64,
+//    64 of 49 tokens in the mean: 18.1, 4 waves 20.6, 8 waves 39.2); else 4 (64 wide: 2 x 10/10, 4096 tokens: 120, 8 waves 141).
+Plan plan(int elem, int D, long long T, int heads, int kv_heads, int n, int max_kv) {
+  const long long group = heads / kv_heads, rows = T * group, units = (rows / 32 + n) * kv_heads;
+  auto tiles = [&](int bm) { return (rows / bm + n) * kv_heads; };
+  const bool few = rows <= 32ll * n, some = rows < 96ll * n;
   Plan r;
-  r.narrow = rows <= 32ll * n && T * heads < (1 << 26) - 4;
-  if (r.narrow && max_kv > 256) {
-    const long long units = (rows / 32 + n) * kv_heads, blocks = units * ((max_kv + 31ll) / 32);
-    r.shares = (int)std::min<long long>(kShares, blocks);
+  r.narrow = few || (elem == 4 ? some || tiles(128) < 128 : max_kv > 512 && tiles(128) < (some ? 120 : 40));
+  if (r.narrow) {
+    if (max_kv > (few || elem == 2 ? 256 : 1024)) r.shares = (int)std::min<long long>(kShares, units * ((max_kv + 31ll) / 32));
+  } else {
+    r.waves = some ? 2 : D == 128 && rows >= 1024ll * n && tiles(256) >= 256 ? 8 : 4;
   }
   return r;
 }
 
 template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) {
-  const Plan r = plan(p.T, p.heads, p.kv_heads, p.seqs.n, p.max_kv);
+  const Plan r = plan(sizeof(T), D, p.T, p.heads, p.kv_heads, p.seqs.n, p.max_kv);
   if (r.narrow) return launch_narrow<T, D>(p, r.shares, s);
-  if constexpr (sizeof(T) == 2 && (D == 64 || D == 128)) {
-    return launch_pipe<D, 64, 8, 4, 2>(p, s);
+  if constexpr (sizeof(T) == 4) {
+    launch<T, D, 4>(p, s);
+  } else if constexpr (D == 128) {
+    r.waves == 8 ? launch_pipe<D, 64, 8, 4, 2>(p, s) : r.waves == 4 ? launch_pipe<D, 32, 4, 5, 2>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
+  } else if constexpr (D == 96) {  // (six waves: whole loads)
+    r.waves == 4 ? launch_pipe<D, 32, 6, 5, 3>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
+  } else if constexpr (D == 64) {
+    r.waves == 4 ? launch_pipe<D, 32, 4, 5, 3>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
   } else {
-    return launch<T, D, 4>(p, s);
+    r.waves == 4 ? launch_pipe<D, 64, 4, 4, 3>(p, s) : launch_pipe<D, 64, 2, 4, 3>(p, s);
   }
 }
 
 }  // namespace
 
-size_t attention_packed_bytes(long long T, int heads, int kv_heads, int D, int n, int max_kv) {
-  const Plan r = plan(T, heads, kv_heads, n, max_kv);
+size_t attention_packed_bytes(int elem, long long T, int heads, int kv_heads, int D, int n, int max_kv) {
+  const Plan r = plan(elem, D, T, heads, kv_heads, n, max_kv);
   Partials part;
   return r.shares ? partials(nullptr, D, r.shares, part) : 0;
 }

@@ -92,7 +92,7 @@ struct PackedAttnParams {
 };
 bool attention_packed_dim(int D);
 // Workspace bytes (0: none).
-size_t attention_packed_bytes(long long T, int heads, int kv_heads, int D, int n, int max_kv);
+size_t attention_packed_bytes(int elem, long long T, int heads, int kv_heads, int D, int n, int max_kv);
 template <typename T> void attention_packed(const PackedAttnParams& p, int D, hipStream_t s);
 
 }  // namespace dn
