@@ -74,7 +74,7 @@ template <int G> __device__ __forceinline__ float group_sum(float v) {
 }
 
 template <typename T, int G, bool HALVES, bool NORM, int HC>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int chunks) {
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int chunks, int width) {
   typedef typename Quad<T>::raw raw;
   const int c = threadIdx.x & (G - 1);
   const bool lane_in = 8 * c < p.D;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
   }
   for (long long u = (long long)blockIdx.x * (kThreads / G) + threadIdx.x / G; u < units; u += step) {
     const long long t = u / chunks;
-    const int h0 = (int)(u - t * chunks) * HC;
+    const int h0 = (int)(u - t * chunks) * width, h1 = min(h0 + width, all);  // width <= HC
     // the rows of keys and values this one goes to
     long long row = t;
     if (p.seqs.n) {
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
 #pragma unroll
       for (int j = 0; j < HC; ++j) {
         const int h = h0 + j;
-        if (h < all) {
+        if (h < h1) {
           const int hk = h - p.heads, hv = hk - p.kv_heads;
           const T* src = hk < 0   ? static_cast<const T*>(p.q) + t * p.ldq + h * p.D
                          : hv < 0 ? static_cast<const T*>(p.k) + t * p.ldk + hk * p.D
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
 #pragma unroll
     for (int j = 0; j < HC; ++j) {
       const int h = h0 + j;
-      if (h >= all) break;
+      if (h >= h1) break;
       const int hk = h - p.heads, hv = hk - p.kv_heads;
       T* dst = hk < 0   ? static_cast<T*>(p.qo) + t * p.ldqo + h * p.D
                : hv < 0 ? static_cast<T*>(p.ko) + row * p.ldko + hk * p.D
@@ -181,17 +181,27 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
 
 template <typename T, int G, bool HALVES, bool NORM, int HC> void launch(const RotaryParams& p, hipStream_t s) {
   const int all = p.heads + p.kv_heads + p.v_heads;
-  const int chunks = (all + HC - 1) / HC;
+  const int chunks = (all + HC - 1) / HC, width = (all + chunks - 1) / chunks;
   const long long blocks = (p.T * chunks + kThreads / G - 1) / (kThreads / G);
   hipLaunchKernelGGL((rotary_kernel<T, G, HALVES, NORM, HC>), dim3((unsigned)std::min(blocks, 1ll << 20)), dim3(kThreads), 0, s,
-                     p, chunks);
+                     p, chunks, width);
   DN_HIP(hipGetLastError());
 }
 
+// Heads a group takes in turn, by the waves that one head each would make: few rows want every lane at once, many share
+// angles and the search for the sequence and keep more loads in flight. Measured, us, of 1, 2, 4 and 8 heads:
+// 576 waves (48 tokens, 32 + 8 + 8 heads of 128) 3.6, 3.9, 4.6, 6.1; 2,250 (750 tokens, 4 + 1 + 1 of 256, fp32) 5.2, 4.8, 5.1,
+// 6.1; 10,240 (8192 tokens, 10 of 64) 7.9, 6.0, 5.5, 5.9; 327,600 (32,760 tokens, 20 + 20 of 128) 212, 141, 123, 126; up to
+// eight heads in all in one piece (4 + 1 + 1 of 80, 19 k tokens) 33.0, 22.9, 21.1, 16.5.
 template <typename T, int G, bool HALVES, bool NORM> void launch_heads(const RotaryParams& p, hipStream_t s) {
-  const long long waves = p.T * (p.heads + p.kv_heads + p.v_heads) * G / 64;
-  if (waves >= 4 * 4096)
+  const int all = p.heads + p.kv_heads + p.v_heads;
+  const long long waves = p.T * all * G / 64;
+  if (waves >= 8192 && all > 4 && all <= 8)
+    launch<T, G, HALVES, NORM, 8>(p, s);
+  else if (waves >= 4096)
     launch<T, G, HALVES, NORM, 4>(p, s);
+  else if (waves >= 1024)
+    launch<T, G, HALVES, NORM, 2>(p, s);
   else
     launch<T, G, HALVES, NORM, 1>(p, s);
 }

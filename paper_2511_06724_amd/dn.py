@@ -556,23 +556,32 @@ def _head_types():
     return {torch.float32: DN_FP32, torch.bfloat16: DN_BF16}
 
 
+@functools.lru_cache(maxsize=None)
+def _plain_types():
+    import torch
+    return torch.int32, torch.float32
+
+
 def _heads(x, name):
-    """(dtype, row stride, rows, heads, head_dim) of a tensor of heads: [rows, heads, head_dim] with dense heads
-    side by side (a slice of a wider projection output is one)."""
-    if x.dim() != 3:
+    """(address, row stride, dtype, shape) of a tensor of heads: [rows, heads, head_dim] with dense heads side by
+    side (a slice of a wider projection output is one)."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3:
         raise ValueError(f"{name}: a tensor [rows, heads, head_dim] is needed")
-    (rows, heads, dim), (ld, sh, sd) = x.shape, x.stride()
-    if (dim > 1 and sd != 1) or (heads > 1 and sh != dim):
+    dim = shape[2]
+    if (stride[2] != 1 and dim > 1) or (stride[1] != dim and shape[1] > 1):
         raise ValueError(f"{name}: the heads of a row must be dense, side by side")
     dt = _head_types().get(x.dtype)
     if dt is None:
         raise ValueError(f"{name}: heads must be float32 or bfloat16")
-    return dt, heads * dim if rows == 1 and ld < heads * dim else ld, rows, heads, dim
+    ld = stride[0]
+    return x.data_ptr(), shape[1] * dim if shape[0] == 1 and ld < shape[1] * dim else ld, dt, shape
 
 
 def _dense(t, dtype, shape, name):
-    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: a dense {dtype} tensor {list(shape)} is needed")
+    return t.data_ptr()
 
 
 class Sequences:
@@ -588,6 +597,7 @@ class Sequences:
         self.n, self.max_kv_len = n, int(max_kv_len)
         self._keep = (q_start, kv_start, kv_len)
         self._c = _Sequences(n, self.max_kv_len, _ptr(q_start), _ptr(kv_start), _ptr(kv_len))
+        self.ref = C.byref(self._c)
 
 
 def rope_freqs(axis_dims, theta=10000.0, per_axis=True):
@@ -612,7 +622,8 @@ class RopeTable:
             raise ValueError("rope_table: one frequency per rotated pair is needed")
         self.rot_dim, self.n_axes = sum(self.axis_dims), len(self.axis_dims)
         self.data = torch.empty(DN_ROPE_TABLE_BYTES, device=device, dtype=torch.uint8)
-        _check(lib.dn_rope_table(f.ctypes.data, dims.ctypes.data, self.n_axes, _ptr(self.data), _stream(stream)))
+        self.address = self.data.data_ptr()
+        _check(lib.dn_rope_table(f.ctypes.data, dims.ctypes.data, self.n_axes, self.address, _stream(stream)))
 
 
 def rope_table(axis_dims, theta=10000.0, per_axis=True, freqs=None, device="cuda", stream=None):
@@ -622,21 +633,21 @@ def rope_table(axis_dims, theta=10000.0, per_axis=True, freqs=None, device="cuda
 
 
 def _rotation(table, pos, rows, pairing, name):
-    import torch
-    _dense(pos, torch.int32, (rows, table.n_axes), f"{name}: pos")
-    return C.byref(_Rotation(_ptr(table.data), _ptr(pos), table.n_axes, table.rot_dim, pairing))
+    return C.byref(_Rotation(table.address, _dense(pos, _plain_types()[0], (rows, table.n_axes), f"{name}: pos"), table.n_axes,
+                             table.rot_dim, pairing))
 
 
 def op_rope(x, pos, table, y=None, pairing=DN_ROPE_PAIRS, stream=None):
     """Rotates the heads of x [rows, heads, head_dim] to pos int32 [rows, axes] (into y, a new tensor, or x itself)."""
-    import torch
-    dt, ldx, rows, heads, dim = _heads(x, "op_rope")
+    src, ldx, dt, shape = _heads(x, "op_rope")
     if y is None:
-        y = torch.empty(rows, heads, dim, device=x.device, dtype=x.dtype)
-    yt, ldy, *shape = _heads(y, "op_rope: y")
-    if yt != dt or shape != [rows, heads, dim]:
+        import torch
+        y = torch.empty(shape, device=x.device, dtype=x.dtype)
+    dst, ldy, yt, y_shape = _heads(y, "op_rope: y")
+    if yt != dt or y_shape != shape:
         raise ValueError("op_rope: y must have the type and shape of x")
-    _check(lib.dn_op_rope(dt, _ptr(x), ldx, _ptr(y), ldy, rows, heads, dim, _rotation(table, pos, rows, pairing, "op_rope"),
+    rows, heads, dim = shape
+    _check(lib.dn_op_rope(dt, src, ldx, dst, ldy, rows, heads, dim, _rotation(table, pos, rows, pairing, "op_rope"),
                           _stream(stream)))
     return y
 
@@ -645,30 +656,31 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, eps, pos, table, q_out, k_out, v=None,
                     pairing=DN_ROPE_PAIRS, stream=None):
     """RMS norm and rotation of every head of q and k [rows, heads, head_dim] into q_out and k_out, v copied to v_out;
     with seqs (Sequences) k_out and v_out are caches whose rows the sequences own."""
-    import torch
     name = "op_qk_norm_rope"
-    dt, ldq, rows, heads, dim = _heads(q, f"{name}: q")
-    kt, ldk, k_rows, kv_heads, k_dim = _heads(k, f"{name}: k")
-    qot, ldqo, *q_shape = _heads(q_out, f"{name}: q_out")
-    kot, ldko, out_rows, *ko_shape = _heads(k_out, f"{name}: k_out")
-    if (kt, qot, kot) != (dt, dt, dt) or (k_rows, k_dim) != (rows, dim) or q_shape != [rows, heads, dim]:
+    pq, ldq, dt, shape = _heads(q, name)
+    pk, ldk, kt, k_shape = _heads(k, name)
+    pqo, ldqo, qot, qo_shape = _heads(q_out, name)
+    pko, ldko, kot, ko_shape = _heads(k_out, name)
+    rows, heads, dim = shape
+    if kt != dt or qot != dt or kot != dt or k_shape[0] != rows or k_shape[2] != dim or qo_shape != shape:
         raise ValueError(f"{name}: types, rows and head widths of q, k and their outputs must agree")
-    if ko_shape != [kv_heads, dim] or (seqs is None and out_rows != rows):
+    if (ko_shape[1:] if seqs is not None else ko_shape) != (k_shape[1:] if seqs is not None else k_shape):
         raise ValueError(f"{name}: k_out must have the heads of k, and its rows where there are no sequences")
+    pv = pvo = None
     ldv = ldvo = 0
     if (v is None) != (v_out is None):
         raise ValueError(f"{name}: values and their output go together")
     if v is not None:
-        vt, ldv, *v_shape = _heads(v, f"{name}: v")
-        vot, ldvo, *vo_shape = _heads(v_out, f"{name}: v_out")
-        if (vt, vot) != (dt, dt) or v_shape != [rows, kv_heads, dim] or vo_shape != [out_rows, kv_heads, dim]:
+        pv, ldv, vt, v_shape = _heads(v, name)
+        pvo, ldvo, vot, vo_shape = _heads(v_out, name)
+        if vt != dt or vot != dt or v_shape != k_shape or vo_shape != ko_shape:
             raise ValueError(f"{name}: values must have the type and shape of the keys, and so must their output")
-    _dense(q_gain, torch.float32, (dim,), f"{name}: q_gain")
-    _dense(k_gain, torch.float32, (dim,), f"{name}: k_gain")
-    _check(lib.dn_op_qk_norm_rope(dt, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, rows, heads, kv_heads, dim, _ptr(q_gain),
-                                  _ptr(k_gain), eps, _rotation(table, pos, rows, pairing, name),
-                                  C.byref(seqs._c) if seqs is not None else None, _ptr(q_out), ldqo, _ptr(k_out), ldko,
-                                  _ptr(v_out), ldvo, out_rows, _stream(stream)))
+    f32 = _plain_types()[1]
+    _check(lib.dn_op_qk_norm_rope(dt, pq, ldq, pk, ldk, pv, ldv, rows, heads, k_shape[1], dim,
+                                  _dense(q_gain, f32, (dim,), "op_qk_norm_rope: q_gain"),
+                                  _dense(k_gain, f32, (dim,), "op_qk_norm_rope: k_gain"), eps,
+                                  _rotation(table, pos, rows, pairing, name), None if seqs is None else seqs.ref, pqo, ldqo, pko,
+                                  ldko, pvo, ldvo, ko_shape[0], _stream(stream)))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -680,7 +692,7 @@ def _attention_packed_bytes(dtype, rows, heads, kv_heads, dim, n, max_kv_len):
 
 def attention_packed_bytes(q, k, seqs):
     """Workspace bytes of op_attention_packed for tensors like q and k (0: none is needed)."""
-    dt, _, rows, heads, dim = _heads(q, "attention_packed_bytes: q")
+    _, _, dt, (rows, heads, dim) = _heads(q, "attention_packed_bytes: q")
     return _attention_packed_bytes(dt, rows, heads, k.shape[1], dim, seqs.n, seqs.max_kv_len)
 
 
@@ -688,18 +700,20 @@ def op_attention_packed(q, k, v, o, seqs, causal=True, scale=None, ws=None, stre
     """Attention of packed sequences: q, o [rows, heads, head_dim], k, v [kv_rows, kv_heads, head_dim]; scale: default
     head_dim^-1/2; ws: uint8, attention_packed_bytes."""
     name = "op_attention_packed"
-    dt, ldq, rows, heads, dim = _heads(q, f"{name}: q")
-    kt, ldk, *kv = _heads(k, f"{name}: k")
-    vt, ldv, *v_shape = _heads(v, f"{name}: v")
-    ot, ldo, *o_shape = _heads(o, f"{name}: o")
-    if (kt, vt, ot) != (dt, dt, dt) or o_shape != [rows, heads, dim] or kv != v_shape or kv[2] != dim:
+    pq, ldq, dt, shape = _heads(q, name)
+    pk, ldk, kt, k_shape = _heads(k, name)
+    pv, ldv, vt, v_shape = _heads(v, name)
+    po, ldo, ot, o_shape = _heads(o, name)
+    rows, heads, dim = shape
+    kv_rows, kv_heads, k_dim = k_shape
+    if kt != dt or vt != dt or ot != dt or o_shape != shape or v_shape != k_shape or k_dim != dim:
         raise ValueError(f"{name}: types and shapes of q, k, v and o must agree")
-    need = _attention_packed_bytes(dt, rows, heads, kv[1], dim, seqs.n, seqs.max_kv_len)
+    need = _attention_packed_bytes(dt, rows, heads, kv_heads, dim, seqs.n, seqs.max_kv_len)
     if ws is not None:
-        _buffer(ws, need, f"{name} workspace")
-    _check(lib.dn_op_attention_packed(dt, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(o), ldo, rows, kv[0], heads, kv[1], dim,
-                                      C.byref(seqs._c), int(causal), dim ** -0.5 if scale is None else scale,
-                                      _ptr(ws) if need else None, _stream(stream)))
+        _buffer(ws, need, name)
+    _check(lib.dn_op_attention_packed(dt, pq, ldq, pk, ldk, pv, ldv, po, ldo, rows, kv_rows, heads, kv_heads, dim, seqs.ref,
+                                      1 if causal else 0, dim ** -0.5 if scale is None else scale,
+                                      ws.data_ptr() if need and ws is not None else None, _stream(stream)))
 
 
 def packed_weight_elems(dtype, N, K):

@@ -318,6 +318,40 @@ def test_attention_long(dtype, q_len, kv_len, hq, hk, dim):
         assert torch.equal(b.run(causal), first), "the same inputs, the same bits"
 
 
+# One batch for every way a call is run: tiles of 2, 4 and 8 waves, units of 32 rows whole and divided, by lengths and heads.
+WAYS = [(dn.DN_BF16, 128, [40, 90, 33], [40, 90, 33], 3, 3), (dn.DN_BF16, 64, [70, 1, 50], [200, 80, 50], 4, 2),
+        (dn.DN_BF16, 96, [40, 60], [41, 77], 2, 1), (dn.DN_BF16, 32, [90, 20], [90, 400], 2, 2),
+        (dn.DN_BF16, 128, [300, 129], [300, 400], 4, 4), (dn.DN_BF16, 64, [450, 2], [500, 2], 2, 2),
+        (dn.DN_BF16, 96, [320, 190], [330, 190], 1, 1), (dn.DN_BF16, 32, [257, 200], [257, 260], 4, 2),
+        (dn.DN_BF16, 128, [1030, 1100], [1030, 1500], 52, 52), (dn.DN_BF16, 128, [130], [3000], 8, 1), (dn.DN_BF16, 64, [60, 64], [2000, 900], 2, 2),
+        (dn.DN_FP32, 64, [40, 300], [40, 900], 4, 2), (dn.DN_FP32, 128, [200], [1800], 4, 2), (dn.DN_FP32, 96, [1030, 900], [1100, 900], 8, 8),
+        (dn.DN_FP32, 32, [1000], [1000], 20, 20), (dn.DN_FP32, 128, [1000, 1], [1000, 70], 16, 16), (dn.DN_FP32, 64, [700, 800], [720, 800], 12, 12)]
+
+
+@pytest.mark.parametrize("way", range(len(WAYS)))
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_each_way(way, causal):
+    dtype, dim, q_len, kv_len, hq, hk = WAYS[way]
+    announce(f"way {way}: {dtype} {dim} {q_len} {kv_len} {hq}/{hk} {causal}")
+    b = Batch(q_len, kv_len, hq, hk, dim, dtype, seed=way)
+    first = b.run(causal).clone()
+    b.check(causal, rows=np.array([0, 1, 17, 31, 32, 63, 64, 100, 127, 128, 255, 256, 300, 1029, 1099]))
+    assert torch.equal(b.run(causal), first)
+    # values that are not finite, in the last key of the last sequence: no other sequence or earlier row sees it
+    m = kv_len[-1]
+    b.v[b.start[-1] + m - 1] = float("nan")
+    b.run(causal)
+    last = b.total - 1
+    assert torch.isnan(b.o[last]).all()
+    b.v[b.start[-1] + m - 1] = 0.0
+    for s, (at, ref, tol) in enumerate(b.expect(causal, rows=np.array([0, 1, 31, 200]))):
+        if s < len(q_len) - 1:
+            close(host(b.o)[at], ref, tol)
+        elif causal:
+            keep = at < last
+            close(host(b.o)[at[keep]], ref[keep], tol[keep])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("n,m,group", [(300, 300, 1), (1, 300, 4), (130, 1000, 2), (9, 2500, 8), (1, 20000, 1)])

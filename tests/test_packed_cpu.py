@@ -116,7 +116,7 @@ def test_binding_refuses_other_types_and_shapes():
 
 def test_binding_refuses_positions_and_gains():
     class Table:
-        n_axes, rot_dim, data = 2, 64, t(2048, dtype=torch.uint8)
+        n_axes, rot_dim, address = 2, 64, P
     x = t(5, 4, 64)
     for pos in (t(5, 2), t(5, 3, dtype=torch.int32), t(4, 2, dtype=torch.int32), t(5, 4, dtype=torch.int32)[:, ::2]):
         with pytest.raises(ValueError):
