@@ -1060,8 +1060,7 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
 
 // Joins the parts of a divided unit: a workgroup per row, whose wave w takes parts w, w + kJoin, ..; then the waves' sums
 // in order. A lane holds the statistics of one part and D / 64 of the row's values.
-constexpr int kJoin = 8;
-template <typename T, int D> __global__ __launch_bounds__(64 * kJoin) void join_kernel(PackedAttnParams p, int group, Partials part) {
+template <typename T, int D, int kJoin> __global__ __launch_bounds__(64 * kJoin) void join_kernel(PackedAttnParams p, int group, Partials part) {
   constexpr int E = (D + 63) / 64;
   __shared__ float s_v[kJoin][E * 64], s_top[kJoin], s_sum[kJoin];
   const int w0 = blockIdx.x, lane = threadIdx.x & 63;
@@ -1138,11 +1137,11 @@ size_t partials(void* ws, int D, int shares, Partials& r) {
 // 128: 181 us, with two waves and 512 200, with four and 256 212. Others: four waves on a unit.
 constexpr int kShares = 1024;
 
-// Of few blocks the shares are fewer: a block takes a wave about 1 us and a part takes the join about 0.04 us, and
-// one unit may have the shares of its key head to itself, so s shares of B blocks take B / s + 0.04 s / kv_heads.
-int shares_of(long long blocks, int kv_heads, long long units) {
-  const long long s = (long long)(5.0 * std::sqrt((double)blocks * kv_heads));
-  return (int)std::min({std::max(s, units), blocks, (long long)kShares});
+// Of few blocks the shares are fewer: a block takes a wave about 1 us (fp32 2.5) and a part takes the join about 0.04 us.
+// s shares of B blocks, of which the largest unit has `most`, take t B / s + 0.04 s most / B.
+int shares_of(long long blocks, long long most, long long units, int elem) {
+  const double s = (elem == 2 ? 5.0 : 8.0) * blocks / std::sqrt((double)most);
+  return (int)std::min<long long>({std::max((long long)std::min(s, 1e9), units), blocks, kShares});
 }
 
 template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int shares, hipStream_t s) {
@@ -1153,11 +1152,15 @@ template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int s
     partials(p.ws, D, shares, part);
     // the tensors' rows bound the blocks, too
     const long long blocks = (p.kv_rows / 32 + p.seqs.n) * p.kv_heads * ((rows + 32ll * p.seqs.n - 1) / (32ll * p.seqs.n));
-    shares = std::min(shares, shares_of(blocks, p.kv_heads, (rows / 32 + p.seqs.n) * p.kv_heads));
+    const long long most = std::min(blocks, (p.max_kv + 31ll) / 32);
+    shares = std::min(shares, shares_of(blocks, most, (rows / 32 + p.seqs.n) * p.kv_heads, sizeof(T)));
     hipLaunchKernelGGL((packed_narrow_kernel<T, D, 1, R, true>), dim3(shares), dim3(64), 0, s, p, (int)group, shares, part);
     DN_HIP(hipGetLastError());
     const long long per = std::min<long long>(32, (rows + p.seqs.n - 1) / p.seqs.n);  // rows of a unit, in the mean
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3(shares, (unsigned)per), dim3(64 * kJoin), 0, s, p, (int)group, part);
+    if (shares * most <= 4 * blocks)  // (up to four parts of the largest unit)
+      hipLaunchKernelGGL((join_kernel<T, D, 2>), dim3(shares, (unsigned)per), dim3(128), 0, s, p, (int)group, part);
+    else
+      hipLaunchKernelGGL((join_kernel<T, D, 8>), dim3(shares, (unsigned)per), dim3(512), 0, s, p, (int)group, part);
   } else {
     constexpr int NW = D * sizeof(T) > 256 ? 2 : 4;
     const long long slots = rows / 32 + p.seqs.n;
