@@ -817,7 +817,7 @@ struct Walk {
 };
 
 template <typename T, int D, int NW, int R, bool DIVIDED>
-__global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams p, int group, int shares, Partials part) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) <= 64 ? 2 : 1))) void packed_narrow_kernel(PackedAttnParams p, int group, int shares, Partials part) {
   using MM = Mma<T>;
   using BL = Block<T, D>;
   constexpr int NV = BL::CH / 2;             // 16-byte operands of a K or Q row per lane
@@ -1058,20 +1058,16 @@ __global__ __launch_bounds__(64 * NW) void packed_narrow_kernel(PackedAttnParams
   }
 }
 
-// Joins the parts of a divided unit: a workgroup per row, whose wave w takes parts w, w + kJoin, ..; then the waves' sums
-// in order. A lane holds the statistics of one part and D / 64 of the row's values.
-template <typename T, int D, int kJoin> __global__ __launch_bounds__(64 * kJoin) void join_kernel(PackedAttnParams p, int group, Partials part) {
-  constexpr int E = (D + 63) / 64;
-  __shared__ float s_v[kJoin][E * 64], s_top[kJoin], s_sum[kJoin];
-  const int w0 = blockIdx.x, lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const DividedUnit u = part.unit[w0];
-  const int n = u.last - w0 + 1;
-  for (int r = blockIdx.y; r < u.rows; r += gridDim.y) {
+// A row of a divided unit from its parts first, first + step, ..: reference maximum, row sum and this lane's D / 64 values
+// against it. A lane holds the statistics of one part.
+template <int D> struct JoinedRow {
+  static constexpr int E = (D + 63) / 64;
+  float top = kLowest, sum = 0.f, v[E] = {};
+  __device__ __forceinline__ void add(const Partials& part, int w0, int n, int r, int first, int step) {
+    const int lane = threadIdx.x & 63;
     auto at = [&](int k) { return (2ll * (w0 + k) + (k == 0 ? 1 : 0)) * 32 + r; };
-    float sum = 0.f, v[E] = {}, top = kLowest;
-    for (int c = wave; c < n; c += 64 * kJoin) {
-      const int mine = c + lane * kJoin;
+    for (int c = first; c < n; c += 64 * step) {
+      const int mine = c + lane * step;
       const float2 ml = mine < n ? part.ml[at(mine)] : make_float2(kLowest, 0.f);
       const float up = fmaxf(top, wave_max(ml.x)), alpha = fast_exp2(top - up);
       top = up;
@@ -1079,41 +1075,73 @@ template <typename T, int D, int kJoin> __global__ __launch_bounds__(64 * kJoin)
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] *= alpha;
       const float f = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top), fl = f * ml.y;
-      const int cnt = min(64, (n - c + kJoin - 1) / kJoin);
+      const int cnt = min(64, (n - c + step - 1) / step);
 #pragma unroll 8
       for (int k = 0; k < cnt; ++k) {
         const float fk = __shfl(f, k, 64);
         sum += __shfl(fl, k, 64);
-        const float* o = part.o + at(c + k * kJoin) * D;
+        const float* o = part.o + at(c + k * step) * D;
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] += fk * o[min(e * 64 + lane, D - 1)];  // (without a branch: loads side by side)
       }
     }
+  }
+  template <typename T> __device__ __forceinline__ void store(const PackedAttnParams& p, int group, const DividedUnit& u, int r) const {
+    const int lane = threadIdx.x & 63, row = u.row0 + r, token = row / group;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    T* o = static_cast<T*>(p.o) + (u.q0 + token) * p.ldo + (long long)(u.kvh * group + row - token * group) * D;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(v[e] * inv);
+  }
+};
+
+// Joins units of few parts: four waves take the rows of the units that four shares begin in turn.
+template <typename T, int D> __global__ __launch_bounds__(256) void join_rows_kernel(PackedAttnParams p, int group, int shares, Partials part) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int before = 0;
+  for (int w0 = blockIdx.x * 4; w0 < min(shares, (int)blockIdx.x * 4 + 4); ++w0) {
+    const DividedUnit u = part.unit[w0];
+    for (int r = (wave - before) & 3; r < u.rows; r += 4) {
+      JoinedRow<D> row;
+      row.add(part, w0, u.last - w0 + 1, r, 0, 1);
+      row.template store<T>(p, group, u, r);
+    }
+    before += u.rows;
+  }
+}
+
+// Joins units of many parts: a workgroup per row, whose wave w takes parts w, w + kJoin, ..; then the waves' sums in order.
+constexpr int kJoin = 8;
+template <typename T, int D> __global__ __launch_bounds__(64 * kJoin) void join_kernel(PackedAttnParams p, int group, Partials part) {
+  constexpr int E = JoinedRow<D>::E;
+  __shared__ float s_v[kJoin][E * 64], s_top[kJoin], s_sum[kJoin];
+  const int w0 = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const DividedUnit u = part.unit[w0];
+  for (int r = blockIdx.y; r < u.rows; r += gridDim.y) {
+    JoinedRow<D> row;
+    row.add(part, w0, u.last - w0 + 1, r, wave, kJoin);
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_v[wave][e * 64 + lane] = v[e];
+    for (int e = 0; e < E; ++e) s_v[wave][e * 64 + lane] = row.v[e];
     if (lane == 0) {
-      s_top[wave] = top;
-      s_sum[wave] = sum;
+      s_top[wave] = row.top;
+      s_sum[wave] = row.sum;
     }
     __syncthreads();
     if (wave == 0) {
+      JoinedRow<D> all;
 #pragma unroll
-      for (int k = 1; k < kJoin; ++k) top = fmaxf(top, s_top[k]);
-      float total = 0.f, x[E] = {};
+      for (int k = 0; k < kJoin; ++k) all.top = fmaxf(all.top, s_top[k]);
 #pragma unroll
       for (int k = 0; k < kJoin; ++k) {
-        const float f = fast_exp2(s_top[k] - top);
-        total += f * s_sum[k];
+        const float f = fast_exp2(s_top[k] - all.top);
+        all.sum += f * s_sum[k];
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] += f * s_v[k][e * 64 + lane];
+        for (int e = 0; e < E; ++e) all.v[e] += f * s_v[k][e * 64 + lane];
       }
-      const float inv = total != 0.f ? 1.f / total : 0.f;
-      const int row = u.row0 + r, token = row / group;
-      T* o = static_cast<T*>(p.o) + (u.q0 + token) * p.ldo + (long long)(u.kvh * group + row - token * group) * D;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(x[e] * inv);
+      all.template store<T>(p, group, u, r);
     }
   }
 }
@@ -1135,13 +1163,13 @@ size_t partials(void* ws, int D, int shares, Partials& r) {
 
 // Divided calls: one wave a workgroup, up to 1024 of them (four a CU, by their rings): 32 contexts up to 54 k, 32/8 heads of
 // 128: 181 us, with two waves and 512 200, with four and 256 212. Others: four waves on a unit.
-constexpr int kShares = 1024;
+constexpr int most_shares(int row_bytes) { return row_bytes <= 64 ? 2048 : 1024; }
 
 // Of few blocks the shares are fewer: a block takes a wave about 1 us (fp32 2.5) and a part takes the join about 0.04 us.
 // s shares of B blocks, of which the largest unit has `most`, take t B / s + 0.04 s most / B.
-int shares_of(long long blocks, long long most, long long units, int elem) {
+int shares_of(long long blocks, long long most, long long units, int elem, int D) {
   const double s = (elem == 2 ? 5.0 : 8.0) * blocks / std::sqrt((double)most);
-  return (int)std::min<long long>({std::max((long long)std::min(s, 1e9), units), blocks, kShares});
+  return (int)std::min<long long>({std::max((long long)std::min(s, 1e9), units), blocks, most_shares(D * elem)});
 }
 
 template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int shares, hipStream_t s) {
@@ -1153,14 +1181,16 @@ template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int s
     // the tensors' rows bound the blocks, too
     const long long blocks = (p.kv_rows / 32 + p.seqs.n) * p.kv_heads * ((rows + 32ll * p.seqs.n - 1) / (32ll * p.seqs.n));
     const long long most = std::min(blocks, (p.max_kv + 31ll) / 32);
-    shares = std::min(shares, shares_of(blocks, most, (rows / 32 + p.seqs.n) * p.kv_heads, sizeof(T)));
+    shares = std::min(shares, shares_of(blocks, most, (rows / 32 + p.seqs.n) * p.kv_heads, sizeof(T), D));
     hipLaunchKernelGGL((packed_narrow_kernel<T, D, 1, R, true>), dim3(shares), dim3(64), 0, s, p, (int)group, shares, part);
     DN_HIP(hipGetLastError());
     const long long per = std::min<long long>(32, (rows + p.seqs.n - 1) / p.seqs.n);  // rows of a unit, in the mean
-    if (shares * most <= 4 * blocks)  // (up to four parts of the largest unit)
-      hipLaunchKernelGGL((join_kernel<T, D, 2>), dim3(shares, (unsigned)per), dim3(128), 0, s, p, (int)group, part);
+    // up to about 32 parts of the largest unit, and not so few rows that every one can have a workgroup (16/2 x 128, 128 tokens
+    // behind 16 k keys: 98 us, with a workgroup per row 128; 13 single tokens, 1/1 x 96: 14.8 and 10.4)
+    if (shares * per > 1024 && shares * most <= 32 * blocks)
+      hipLaunchKernelGGL((join_rows_kernel<T, D>), dim3((shares + 3) / 4), dim3(256), 0, s, p, (int)group, shares, part);
     else
-      hipLaunchKernelGGL((join_kernel<T, D, 8>), dim3(shares, (unsigned)per), dim3(512), 0, s, p, (int)group, part);
+      hipLaunchKernelGGL((join_kernel<T, D>), dim3(shares, (unsigned)per), dim3(64 * kJoin), 0, s, p, (int)group, part);
   } else {
     constexpr int NW = D * sizeof(T) > 256 ? 2 : 4;
     const long long slots = rows / 32 + p.seqs.n;
@@ -1207,7 +1237,7 @@ Plan plan(int elem, int D, long long T, int heads, int kv_heads, int n, int max_
   Plan r;
   r.narrow = few || (elem == 4 ? some || tiles(128) < 128 : max_kv > 512 && tiles(128) < (some ? 120 : 40));
   if (r.narrow) {
-    if (max_kv > (few || elem == 2 ? 256 : 1024)) r.shares = (int)std::min<long long>(kShares, units * ((max_kv + 31ll) / 32));
+    if (max_kv > (few || elem == 2 ? 256 : 1024)) r.shares = (int)std::min<long long>(most_shares(D * elem), units * ((max_kv + 31ll) / 32));
   } else {
     r.waves = some ? 2 : D == 128 && rows >= 1024ll * n && tiles(256) >= 256 ? 8 : 4;
   }
