@@ -23,10 +23,9 @@
 // probability, independent from key to key), the row sum adds the rounded values.
 //
 // Masked keys carry no value, also if theirs is an infinity or a NaN: 0 * inf in the matrix product
-// would be NaN. Key rows past the range are not read (the last one is, instead), and if the result of
-// a workgroup with a masked tile has a non-finite value, it runs again and takes non-finite values
-// out of masked tiles, adding them back where they are seen (one tile a work unit at most, plus the
-// border of the range).
+// would be NaN. Key rows past the range are not read (the last one is, instead), and if a workgroup's
+// result has a non-finite value, it computes its rows again and takes such values out of the
+// product, adding them where they are seen. That costs nothing where all results are finite.
 #include <algorithm>
 #include <cmath>
 
@@ -38,7 +37,6 @@ namespace {
 
 constexpr int kKT = 64;        // keys per tile
 constexpr float kLazy = 8.0f;  // log2 headroom before the reference maximum moves
-typedef __attribute__((address_space(1))) void gbl_void_t;
 constexpr float kLowest = -3.402823466e38f;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -49,21 +47,40 @@ struct Unit {
   long long q0, k0;  // first packed row, first key row
 };
 
-// The unit of a slot, by a whole wave. False: the slot is not used.
+__device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ long long from_lane(long long x, int lane) {
+  return (long long)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// The unit of a slot, by a whole wave. False: the slot is not used. Up to 64 sequences lie in the lanes at once, which
+// saves a load that waits for another.
 template <int BM> __device__ __forceinline__ bool find_unit(const PackedAttnParams& p, int group, long long slot, Unit& u) {
   const int* qs = p.seqs.q_start;
-  const int s = __builtin_amdgcn_readfirstlane(
-      search_group<64>(p.seqs.n, slot, [&](int i) { return (long long)qs[i] * group / BM + i; }));
-  if (s < 0) return false;
-  const int a = __builtin_amdgcn_readfirstlane(qs[s]), b = __builtin_amdgcn_readfirstlane(qs[s + 1]);
-  u.len_k = __builtin_amdgcn_readfirstlane(p.seqs.kv_len[s]);
-  const long long k0 = p.seqs.kv_start[s];
-  u.k0 = (long long)__builtin_amdgcn_readfirstlane((int)(k0 >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)k0);
+  auto place = [&](int q, int i) { return (long long)q * group / BM + i; };
+  int s, a, b;
+  if (p.seqs.n <= 64) {
+    const int i = min((int)(threadIdx.x & 63), p.seqs.n - 1);
+    const int qa = qs[i], qb = qs[i + 1], len = p.seqs.kv_len[i];
+    const long long k0 = p.seqs.kv_start[i];
+    s = __popcll(__ballot((int)(threadIdx.x & 63) < p.seqs.n && place(qa, i) <= slot)) - 1;
+    if (s < 0) return false;
+    a = from_lane(qa, s);
+    b = from_lane(qb, s);
+    u.len_k = from_lane(len, s);
+    u.k0 = from_lane(k0, s);
+  } else {
+    s = __builtin_amdgcn_readfirstlane(search_group<64>(p.seqs.n, slot, [&](int i) { return place(qs[i], i); }));
+    if (s < 0) return false;
+    a = __builtin_amdgcn_readfirstlane(qs[s]);
+    b = __builtin_amdgcn_readfirstlane(qs[s + 1]);
+    u.len_k = __builtin_amdgcn_readfirstlane(p.seqs.kv_len[s]);
+    u.k0 = from_lane(p.seqs.kv_start[s], 0);
+  }
   if (a < 0 || b <= a || b > p.T || u.len_k < 0 || u.k0 < 0 || u.k0 > p.kv_rows - u.len_k) return false;
   u.q0 = a;
   u.len_q = b - a;
-  const long long rows = (long long)u.len_q * group, row0 = (slot - ((long long)a * group / BM + s)) * BM;
-  if (row0 >= rows) return false;
+  const long long rows = (long long)u.len_q * group, row0 = (slot - place(a, s)) * BM;
+  if (row0 < 0 || row0 >= rows) return false;  // (below: starts that are not in order)
   u.rows = (int)rows;
   u.row0 = (int)row0;
   return true;
@@ -248,21 +265,19 @@ __device__ __forceinline__ void careful_rows(const PackedAttnParams& p, const Un
   }
 }
 
-// Any head dim and type: key tiles go through registers into LDS, double-buffered; NW waves of 32 rows.
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void packed_kernel(PackedAttnParams p, int group) {
-  using MM = Mma<T>;
-  using V = Pv<T>;
-  constexpr int BM = 32 * NW;
-  constexpr int NT = 64 * NW;
-  constexpr int VEC = 16 / sizeof(T);
-  constexpr int LD = D + VEC;       // LDS row of a key (elements)
-  constexpr int NS = D / MM::KS;    // matrix steps over the head dim
+// fp32 tiles: four waves of 32 rows, key tiles through registers into LDS, double-buffered. Bound by the fp32 matrix
+// instructions. A lane reads four head dims of K (and held four of Q) at a time, in the same order on both sides.
+template <int D> __global__ __launch_bounds__(256) void packed_f32_kernel(PackedAttnParams p, int group) {
+  using MM = Mma<float>;
+  using V = Pv<float>;
+  constexpr int NW = 4, BM = 32 * NW, NT = 64 * NW;
+  constexpr int LD = D + 4;         // LDS row of a key (elements)
+  constexpr int NV = D / 8;         // 16-byte operands of a row per lane
   constexpr int DB = D / 32;
-  constexpr int CH = D / VEC;       // 16-byte pieces per row
-  constexpr int PER = (kKT * CH + NT - 1) / NT;
+  constexpr int CH = D / 4;         // 16-byte pieces per row
+  constexpr int PER = kKT * CH / NT;
   constexpr int STAGE = 2 * kKT * LD;
-  __shared__ __align__(16) T lds[2 * STAGE];
+  __shared__ __align__(16) float lds[2 * STAGE];
 
   Unit u;
   if (!find_unit<BM>(p, group, blockIdx.x, u)) return;
@@ -273,133 +288,122 @@ __global__ __launch_bounds__(64 * NW) void packed_kernel(PackedAttnParams p, int
   const int row = min(first + (lane & 31), u.rows - 1);
   const int token = row / group, head = kvh * group + row - token * group;
   const int lim = limit(p, u, token);
-  const int lim_min = limit(p, u, min(first, u.rows - 1) / group);                // of the wave
-  const int end = limit(p, u, min(u.row0 + BM - 1, u.rows - 1) / group);          // of the workgroup
-
-  const T* qp = static_cast<const T*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D;
-  typename MM::frag qf[NS];
-#pragma unroll
-  for (int s = 0; s < NS; ++s) qf[s] = MM::load(qp + s * MM::KS + half * MM::KPL);
-  const T* kp = static_cast<const T*>(p.k) + u.k0 * p.ldk + (long long)kvh * D;
-  const T* vp = static_cast<const T*>(p.v) + u.k0 * p.ldv + (long long)kvh * D;
-
+  const int lo = limit(p, u, min(first, u.rows - 1) / group);                // the wave's shortest range
+  const int end = limit(p, u, min(u.row0 + BM - 1, u.rows - 1) / group);     // the workgroup's longest
   const int ntiles = (end + kKT - 1) / kKT;
-  f32x16 o[DB];
-  float m_ref, l_run;
+
+  const float* qp = static_cast<const float*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D + half * 4;
+  f32x4 qv[NV];
+#pragma unroll
+  for (int n = 0; n < NV; ++n) qv[n] = __builtin_bit_cast(f32x4, ld16(qp + n * 8));
+  const float* kp = static_cast<const float*>(p.k) + u.k0 * p.ldk + (long long)kvh * D;
+  const float* vp = static_cast<const float*>(p.v) + u.k0 * p.ldv + (long long)kvh * D;
   uint4 rk[PER], rv[PER];
   auto load = [&](int t) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int w = tid + i * NT;
-      if (PER * NT != kKT * CH && w >= kKT * CH) break;
-      const int r = w / CH, c = w - r * CH;
+      const int w = tid + i * NT, r = w / CH, c = w - r * CH;
       const long long key = min(t * kKT + r, end - 1);
-      rk[i] = ld16(kp + key * p.ldk + c * VEC);
-      rv[i] = ld16(vp + key * p.ldv + c * VEC);
+      rk[i] = ld16(kp + key * p.ldk + c * 4);
+      rv[i] = ld16(vp + key * p.ldv + c * 4);
     }
   };
   auto store = [&](int buf) {
-    T* ks = lds + buf * STAGE;
+    float* ks = lds + buf * STAGE;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int w = tid + i * NT;
-      if (PER * NT != kKT * CH && w >= kKT * CH) break;
-      const int r = w / CH, c = w - r * CH;
-      st16(ks + r * LD + c * VEC, rk[i]);
-      st16(ks + kKT * LD + r * LD + c * VEC, rv[i]);
+      const int w = tid + i * NT, r = w / CH, c = w - r * CH;
+      st16(ks + r * LD + c * 4, rk[i]);
+      st16(ks + kKT * LD + r * LD + c * 4, rv[i]);
     }
   };
 
+  f32x16 o[DB];
+  float m = kLowest, l = 0.f;
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-  m_ref = kLowest;
-  l_run = 0.f;
-  {
-    if (ntiles > 0) {
-      load(0);
-      store(0);
-      if (ntiles > 1) load(1);
+  if (ntiles > 0) {
+    load(0);
+    store(0);
+    if (ntiles > 1) load(1);
+  }
+  __syncthreads();
+  for (int t = 0; t < ntiles; ++t) {
+    const int k0 = t * kKT;
+    const float* ks = lds + (t & 1) * STAGE;
+    const float* vs = ks + kKT * LD;
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      f32x4 ka[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        ka[kb] = __builtin_bit_cast(f32x4, ld16(&ks[(kb * 32 + (lane & 31)) * LD + n * 8 + half * 4]));
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[kb] = MM::mma(ka[kb][e], qv[n][e], s[kb]);
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] *= p.scale_log2;
+    if (k0 + kKT > lo) {  // keys past a range
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (k0 + kb * 32 + acc_row(r, lane) >= lim) s[kb][r] = -INFINITY;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = max2(mx, s[kb][r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    if (__any(mx > m + kLazy)) {
+      const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      m = m_new;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[kb][r] = fast_exp2(s[kb][r] - m);
+        l += s[kb][r];
+      }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int c = 0; c < V::STEPS; ++c)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = MM::mma(V::v(vs, LD, kb, c, d * 32, lane), s[kb][c], o[d]);
+    if (t + 1 < ntiles) {
+      store((t + 1) & 1);
+      if (t + 2 < ntiles) load(t + 2);
     }
     __syncthreads();
-    for (int t = 0; t < ntiles; ++t) {
-      const int k0 = t * kKT;
-      const T* ks = lds + (t & 1) * STAGE;
-      const T* vs = ks + kKT * LD;
-      f32x16 s[2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-          s[kb] = MM::mma(MM::load(&ks[(kb * 32 + (lane & 31)) * LD + i * MM::KS + half * MM::KPL]), qf[i], s[kb]);
-      const bool masked = k0 + kKT > lim_min;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] *= p.scale_log2;
-      if (masked) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (k0 + kb * 32 + acc_row(r, lane) >= lim) s[kb][r] = -INFINITY;
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      if (__any(mx > m_ref + kLazy)) {
-        const float m_new = fmaxf(m_ref, mx);
-        const float alpha = fast_exp2(m_ref - m_new);
-        l_run *= alpha;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
-        m_ref = m_new;
-      }
-      float rs = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float e = to_f32(from_f32<T>(fast_exp2(s[kb][r] - m_ref)));
-          s[kb][r] = e;
-          rs += e;
-        }
-      l_run += rs + __shfl_xor(rs, 32, 64);
-      {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int c = 0; c < V::STEPS; ++c) {
-            const typename MM::frag pf = V::p(s[kb], c);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) o[d] = MM::mma(V::v(vs, LD, kb, c, d * 32, lane), pf, o[d]);
-          }
-      }
-      if (t + 1 < ntiles) {
-        store((t + 1) & 1);
-        if (t + 2 < ntiles) load(t + 2);
-      }
-      __syncthreads();
-    }
   }
-  if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds))) 
-    return careful_rows<T, D, NW>(p, u, group, kvh, lds, 0, end, [&](int tok, int h, int d, const f32x16& x, float, float sum) {
-      store_block<T>(row_out<T>(p, u, tok, h, D) + 32 * d, x, sum);
+  l += __shfl_xor(l, 32, 64);  // each half has summed its own keys
+  if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds)))
+    return careful_rows<float, D, NW>(p, u, group, kvh, lds, 0, end, [&](int tok, int h, int d, const f32x16& x, float, float sum) {
+      store_block<float>(row_out<float>(p, u, tok, h, D) + 32 * d, x, sum);
     });
   if (first + (lane & 31) < u.rows) {
-    T* op = row_out<T>(p, u, token, head, D);
+    float* op = row_out<float>(p, u, token, head, D);
 #pragma unroll
-    for (int d = 0; d < DB; ++d) store_block<T>(op + 32 * d, o[d], l_run);
+    for (int d = 0; d < DB; ++d) store_block<float>(op + 32 * d, o[d], l);
   }
 }
 
@@ -770,11 +774,6 @@ struct Partials {
 
 __device__ __forceinline__ int key_blocks(int len) { return max(1, (len + 31) / 32); }  // (one that stores zeros, without keys)
 
-__device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-__device__ __forceinline__ long long from_lane(long long x, int lane) {
-  return (long long)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
-}
-
 // Sequences in order, 64 at a time in the lanes of a wave: blocks of the units (for one key head) before and in each.
 struct Walk {
   int first = 0;             // sequence of lane 0
@@ -817,7 +816,8 @@ struct Walk {
 };
 
 template <typename T, int D, int NW, int R, bool DIVIDED>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) <= 64 ? 2 : 1))) void packed_narrow_kernel(PackedAttnParams p, int group, int shares, Partials part) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) <= 64 ? 2 : 1))) void packed_narrow_kernel(
+    PackedAttnParams p, int group, int shares, Partials part) {
   using MM = Mma<T>;
   using BL = Block<T, D>;
   constexpr int NV = BL::CH / 2;             // 16-byte operands of a K or Q row per lane
@@ -847,214 +847,214 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D * siz
     x1 = blocks * (blockIdx.x + 1) / g;
   }
   while (x0 < x1) {
-  Unit u;
-  int kvh = blockIdx.y, b0 = 0, b1;
-  bool whole = true;
-  long long unit_part = 0;
-  if constexpr (DIVIDED) {
-    kvh = (int)(x0 / per_head);
-    const long long y = x0 - kvh * per_head;
-    if (y < walk.base) walk.restart(p, group);
-    const int i = walk.find(p, group, y);
-    const int qa = from_lane(walk.qa, i);
-    u.q0 = qa;
-    u.len_q = from_lane(walk.qb, i) - qa;
-    u.len_k = from_lane(walk.len, i);
-    u.k0 = from_lane(walk.k0, i);
-    const int nb = key_blocks(u.len_k);
-    const long long in = y - (walk.base + from_lane(walk.incl - walk.cost, i));
-    const int tile = (int)(in / nb);
-    b0 = (int)(in - (long long)tile * nb);
-    b1 = b0 + (int)min((long long)(nb - b0), x1 - x0);
-    u.row0 = tile * 32;
-    u.rows = (int)min((long long)u.len_q * group, u.row0 + 32ll);
-    whole = b0 == 0 && b1 == nb;
-    unit_part = 2ll * blockIdx.x + (b0 == 0 ? 1 : 0);
-    if (b0 == 0 && !whole && tid == 0) {
-      // the last workgroup w with w blocks / g <= the unit's last block
-      const long long blocks = per_head * p.kv_heads, g = min((long long)shares, blocks);
-      part.unit[blockIdx.x] = DividedUnit{u.rows - u.row0, u.row0, kvh, (int)(((x0 + nb) * g - 1) / blocks), u.q0};
-    }
-    x0 += b1 - b0;
-  } else {
-    if (!find_unit<32>(p, group, blockIdx.x, u)) return;
-    u.rows = min(u.rows, u.row0 + 32);
-    b1 = key_blocks(u.len_k);
-    ++x0;
-  }
-
-  const int row = min(u.row0 + r32, u.rows - 1), token = row / group, head = kvh * group + row - token * group;
-  const int lim = limit(p, u, token);
-  const int range = __builtin_amdgcn_readfirstlane(limit(p, u, (u.rows - 1) / group));
-  const int lo = __builtin_amdgcn_readfirstlane(limit(p, u, u.row0 / group));
-  const int end = min(range, b1 * 32);
-  auto emit = [&](int tok, int h, int d, const f32x16& x, float m, float sum) {
-    if (whole) return store_block<T>(row_out<T>(p, u, tok, h, D) + 32 * d, x, sum);
-    float* o = part.o + (unit_part * 32 + r32) * D + 32 * d + 4 * half;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(o + 8 * g) = f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
-    if (d == 0 && half == 0) part.ml[unit_part * 32 + r32] = make_float2(m, sum);
-  };
-
-  const T* qp = static_cast<const T*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D + half * (16 / sizeof(T));
-  uint4 qv[NV];
-#pragma unroll
-  for (int s = 0; s < NV; ++s) qv[s] = ld16(qp + s * (32 / sizeof(T)));
-  const char* kbase = reinterpret_cast<const char*>(static_cast<const T*>(p.k) + u.k0 * p.ldk + (long long)kvh * D);
-  const char* vbase = reinterpret_cast<const char*>(static_cast<const T*>(p.v) + u.k0 * p.ldv + (long long)kvh * D);
-  unsigned char* ring = lds + wave * R * 2 * BL::BYTES;
-  unsigned koff[LW], voff[LW];
-  auto set_offsets = [&](int keys) {  // of a block that has `keys` keys: the rows past them read the last one
-#pragma unroll
-    for (int j = 0; j < LW; ++j) {
-      const int w = j * 64 + lane, r = w / BL::CH, ch = w - r * BL::CH;
-      const unsigned key = (unsigned)min(r, keys - 1) * (unsigned)sizeof(T);
-      koff[j] = key * (unsigned)p.ldk + 16u * BL::k_piece(r, ch);
-      voff[j] = key * (unsigned)p.ldv + 16u * BL::v_piece(r, ch);
-    }
-  };
-  set_offsets(32);
-  auto issue = [&](int b, int slot) {
-    const char* kb = kbase + (long long)b * 32 * p.ldk * (int)sizeof(T);
-    const char* vb = vbase + (long long)b * 32 * p.ldv * (int)sizeof(T);
-    unsigned char* to = ring + slot * 2 * BL::BYTES;
-    const bool partial = (b + 1) * 32 > end;
-    if (partial) set_offsets(end - b * 32);
-#pragma unroll
-    for (int j = 0; j < LW; ++j) dma16_stream(kb, koff[j], (lds_void*)(to + j * 1024));
-#pragma unroll
-    for (int j = 0; j < LW; ++j) dma16_stream(vb, voff[j], (lds_void*)(to + BL::BYTES + j * 1024));
-    if (partial) set_offsets(32);
-  };
-
-  f32x16 o[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-  float m = kLowest, l = 0.f;
-  const int nk = (end + 31) / 32 - b0;                                   // blocks with keys (some rows see)
-  const int mine = nk > wave ? (nk - wave + NW - 1) / NW : 0;            // of the wave
-  if (mine > 0) {
-#pragma unroll
-    for (int i = 0; i < R - 1; ++i) issue(b0 + wave + min(i, mine - 1) * NW, i);
-  }
-  int slot = 0;
-  for (int i = 0; i < mine; ++i) {
-    // reads of the slot that is loaded now are done; past the last block it is loaded again, so that the count of
-    // loads behind a block is the same
-    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0(63));
-    issue(b0 + wave + min(i + R - 1, mine - 1) * NW, slot == 0 ? R - 1 : slot - 1);
-    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((R - 1) * 2 * LW));
-    __builtin_amdgcn_sched_barrier(0);
-    const unsigned char* K = ring + slot * 2 * BL::BYTES;
-    const T* vs = reinterpret_cast<const T*>(K + BL::BYTES);
-    const int k0 = (b0 + wave + i * NW) * 32;
-    f32x16 s;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const uint4 kv = *reinterpret_cast<const uint4*>(K + r32 * BL::RB + BL::k_piece(r32, 2 * n + half) * 16);
-      if constexpr (sizeof(T) == 4) {
-        const f32x4 ka = __builtin_bit_cast(f32x4, kv), qa = __builtin_bit_cast(f32x4, qv[n]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s = MM::mma(ka[e], qa[e], s);
-      } else {
-        s = MM::mma(__builtin_bit_cast(bf16x8, kv), __builtin_bit_cast(bf16x8, qv[n]), s);
+    Unit u;
+    int kvh = blockIdx.y, b0 = 0, b1;
+    bool whole = true;
+    long long unit_part = 0;
+    if constexpr (DIVIDED) {
+      kvh = (int)(x0 / per_head);
+      const long long y = x0 - kvh * per_head;
+      if (y < walk.base) walk.restart(p, group);
+      const int i = walk.find(p, group, y);
+      const int qa = from_lane(walk.qa, i);
+      u.q0 = qa;
+      u.len_q = from_lane(walk.qb, i) - qa;
+      u.len_k = from_lane(walk.len, i);
+      u.k0 = from_lane(walk.k0, i);
+      const int nb = key_blocks(u.len_k);
+      const long long in = y - (walk.base + from_lane(walk.incl - walk.cost, i));
+      const int tile = (int)(in / nb);
+      b0 = (int)(in - (long long)tile * nb);
+      b1 = b0 + (int)min((long long)(nb - b0), x1 - x0);
+      u.row0 = tile * 32;
+      u.rows = (int)min((long long)u.len_q * group, u.row0 + 32ll);
+      whole = b0 == 0 && b1 == nb;
+      unit_part = 2ll * blockIdx.x + (b0 == 0 ? 1 : 0);
+      if (b0 == 0 && !whole && tid == 0) {
+        // the last workgroup w with w blocks / g <= the unit's last block
+        const long long blocks = per_head * p.kv_heads, g = min((long long)shares, blocks);
+        part.unit[blockIdx.x] = DividedUnit{u.rows - u.row0, u.row0, kvh, (int)(((x0 + nb) * g - 1) / blocks), u.q0};
       }
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] *= p.scale_log2;
-    if (k0 + 32 > min(lo, end)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (k0 + acc_row(r, lane) >= min(lim, end)) s[r] = -INFINITY;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    if (__any(mx > m + kLazy)) {
-      const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - m_new);
-      l *= alpha;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
-      m = m_new;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = to_f32(from_f32<T>(fast_exp2(s[r] - m)));
-      l += s[r];
-    }
-    if constexpr (sizeof(T) == 4) {
-      // register 4 g + e: key 8 g + 4 half + e (V is stored as it is)
-#pragma unroll
-      for (int c = 0; c < 16; ++c)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = MM::mma(vs[(8 * (c >> 2) + 4 * half + (c & 3)) * D + d * 32 + r32], s[c], o[d]);
+      x0 += b1 - b0;
     } else {
-      const int vrow = 4 * half + ((lane & 15) >> 2), vcol = (lane & 16) + 4 * (lane & 3);
+      if (!find_unit<32>(p, group, blockIdx.x, u)) return;
+      u.rows = min(u.rows, u.row0 + 32);
+      b1 = key_blocks(u.len_k);
+      ++x0;
+    }
+
+    const int row = min(u.row0 + r32, u.rows - 1), token = row / group, head = kvh * group + row - token * group;
+    const int lim = limit(p, u, token);
+    const int range = __builtin_amdgcn_readfirstlane(limit(p, u, (u.rows - 1) / group));
+    const int lo = __builtin_amdgcn_readfirstlane(limit(p, u, u.row0 / group));
+    const int end = min(range, b1 * 32);
+    auto emit = [&](int tok, int h, int d, const f32x16& x, float m, float sum) {
+      if (whole) return store_block<T>(row_out<T>(p, u, tok, h, D) + 32 * d, x, sum);
+      float* o = part.o + (unit_part * 32 + r32) * D + 32 * d + 4 * half;
 #pragma unroll
-      for (int cc = 0; cc < 2; ++cc) {
-        const bf16x8 pf = Pv<bf16>::p(s, cc);
+      for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(o + 8 * g) = f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
+      if (d == 0 && half == 0) part.ml[unit_part * 32 + r32] = make_float2(m, sum);
+    };
+
+    const T* qp = static_cast<const T*>(p.q) + (u.q0 + token) * p.ldq + (long long)head * D + half * (16 / sizeof(T));
+    uint4 qv[NV];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const int col = d * 32 + vcol, r0 = 16 * cc + vrow;  // rows r0 and r0 + 8 have one xor
-          const unsigned char* a = K + BL::BYTES + r0 * BL::RB + BL::v_piece(r0, col >> 3) * 16 + (col & 7) * 2;
-          const bf16x4 x = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Pv<bf16>::lds_s16x4*)a));
-          const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Pv<bf16>::lds_s16x4*)(a + 8 * BL::RB)));
-          o[d] = MM::mma(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[d]);
+    for (int s = 0; s < NV; ++s) qv[s] = ld16(qp + s * (32 / sizeof(T)));
+    const char* kbase = reinterpret_cast<const char*>(static_cast<const T*>(p.k) + u.k0 * p.ldk + (long long)kvh * D);
+    const char* vbase = reinterpret_cast<const char*>(static_cast<const T*>(p.v) + u.k0 * p.ldv + (long long)kvh * D);
+    unsigned char* ring = lds + wave * R * 2 * BL::BYTES;
+    unsigned koff[LW], voff[LW];
+    auto set_offsets = [&](int keys) {  // of a block that has `keys` keys: the rows past them read the last one
+#pragma unroll
+      for (int j = 0; j < LW; ++j) {
+        const int w = j * 64 + lane, r = w / BL::CH, ch = w - r * BL::CH;
+        const unsigned key = (unsigned)min(r, keys - 1) * (unsigned)sizeof(T);
+        koff[j] = key * (unsigned)p.ldk + 16u * BL::k_piece(r, ch);
+        voff[j] = key * (unsigned)p.ldv + 16u * BL::v_piece(r, ch);
+      }
+    };
+    set_offsets(32);
+    auto issue = [&](int b, int slot) {
+      const char* kb = kbase + (long long)b * 32 * p.ldk * (int)sizeof(T);
+      const char* vb = vbase + (long long)b * 32 * p.ldv * (int)sizeof(T);
+      unsigned char* to = ring + slot * 2 * BL::BYTES;
+      const bool partial = (b + 1) * 32 > end;
+      if (partial) set_offsets(end - b * 32);
+#pragma unroll
+      for (int j = 0; j < LW; ++j) dma16_stream(kb, koff[j], (lds_void*)(to + j * 1024));
+#pragma unroll
+      for (int j = 0; j < LW; ++j) dma16_stream(vb, voff[j], (lds_void*)(to + BL::BYTES + j * 1024));
+      if (partial) set_offsets(32);
+    };
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    float m = kLowest, l = 0.f;
+    const int nk = (end + 31) / 32 - b0;                                   // blocks with keys (some rows see)
+    const int mine = nk > wave ? (nk - wave + NW - 1) / NW : 0;            // of the wave
+    if (mine > 0) {
+#pragma unroll
+      for (int i = 0; i < R - 1; ++i) issue(b0 + wave + min(i, mine - 1) * NW, i);
+    }
+    int slot = 0;
+    for (int i = 0; i < mine; ++i) {
+      // reads of the slot that is loaded now are done; past the last block it is loaded again, so that the count of
+      // loads behind a block is the same
+      __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0(63));
+      issue(b0 + wave + min(i + R - 1, mine - 1) * NW, slot == 0 ? R - 1 : slot - 1);
+      __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((R - 1) * 2 * LW));
+      __builtin_amdgcn_sched_barrier(0);
+      const unsigned char* K = ring + slot * 2 * BL::BYTES;
+      const T* vs = reinterpret_cast<const T*>(K + BL::BYTES);
+      const int k0 = (b0 + wave + i * NW) * 32;
+      f32x16 s;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const uint4 kv = *reinterpret_cast<const uint4*>(K + r32 * BL::RB + BL::k_piece(r32, 2 * n + half) * 16);
+        if constexpr (sizeof(T) == 4) {
+          const f32x4 ka = __builtin_bit_cast(f32x4, kv), qa = __builtin_bit_cast(f32x4, qv[n]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = MM::mma(ka[e], qa[e], s);
+        } else {
+          s = MM::mma(__builtin_bit_cast(bf16x8, kv), __builtin_bit_cast(bf16x8, qv[n]), s);
         }
       }
-    }
-    slot = slot == R - 1 ? 0 : slot + 1;
-  }
-  __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0(0));
-  l += __shfl_xor(l, 32, 64);
-  if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds))) {
-    __syncthreads();
-    careful_rows<T, D, NW>(p, u, group, kvh, reinterpret_cast<T*>(lds), b0 * 32, end, emit);
-    __syncthreads();
-    continue;
-  }
-  __syncthreads();
-
-  // the waves' results in order: thread (unit w of 32 values d, lane) sums over the waves
-  float* so = reinterpret_cast<float*>(lds);         // [wave][DB][16][64]
-  float* sm = so + NW * DB * 16 * 64;                // [wave][32] m, then [wave][32] l
+      float mx = -INFINITY;
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+      for (int r = 0; r < 16; ++r) s[r] *= p.scale_log2;
+      if (k0 + 32 > min(lo, end)) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) so[((wave * DB + d) * 16 + r) * 64 + lane] = o[d][r];
-  if (half == 0) {
-    sm[wave * 32 + r32] = m;
-    sm[NW * 32 + wave * 32 + r32] = l;
-  }
-  __syncthreads();
-  if (u.row0 + r32 < u.rows) {
-    float top = sm[r32], sum = 0.f, f[NW];
+        for (int r = 0; r < 16; ++r)
+          if (k0 + acc_row(r, lane) >= min(lim, end)) s[r] = -INFINITY;
+      }
 #pragma unroll
-    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w * 32 + r32]);
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      if (__any(mx > m + kLazy)) {
+        const float m_new = fmaxf(m, mx), alpha = fast_exp2(m - m_new);
+        l *= alpha;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      f[w] = fast_exp2(sm[w * 32 + r32] - top);
-      sum += f[w] * sm[NW * 32 + w * 32 + r32];
-    }
-    for (int d = wave; d < DB; d += NW) {
-      f32x16 x;
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+        m = m_new;
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        x[r] = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) x[r] += f[w] * so[((w * DB + d) * 16 + r) * 64 + lane];
+        s[r] = to_f32(from_f32<T>(fast_exp2(s[r] - m)));
+        l += s[r];
       }
-      emit(token, head, d, x, top, sum);
+      if constexpr (sizeof(T) == 4) {
+        // register 4 g + e: key 8 g + 4 half + e (V is stored as it is)
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[d] = MM::mma(vs[(8 * (c >> 2) + 4 * half + (c & 3)) * D + d * 32 + r32], s[c], o[d]);
+      } else {
+        const int vrow = 4 * half + ((lane & 15) >> 2), vcol = (lane & 16) + 4 * (lane & 3);
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc) {
+          const bf16x8 pf = Pv<bf16>::p(s, cc);
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            const int col = d * 32 + vcol, r0 = 16 * cc + vrow;  // rows r0 and r0 + 8 have one xor
+            const unsigned char* a = K + BL::BYTES + r0 * BL::RB + BL::v_piece(r0, col >> 3) * 16 + (col & 7) * 2;
+            const bf16x4 x = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Pv<bf16>::lds_s16x4*)a));
+            const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Pv<bf16>::lds_s16x4*)(a + 8 * BL::RB)));
+            o[d] = MM::mma(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[d]);
+          }
+        }
+      }
+      slot = slot == R - 1 ? 0 : slot + 1;
     }
-  }
-  __syncthreads();
+    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0(0));
+    l += __shfl_xor(l, 32, 64);
+    if (any_not_finite<DB, NW>(o, reinterpret_cast<int*>(lds))) {
+      __syncthreads();
+      careful_rows<T, D, NW>(p, u, group, kvh, reinterpret_cast<T*>(lds), b0 * 32, end, emit);
+      __syncthreads();
+      continue;
+    }
+    __syncthreads();
+
+    // the waves' results in order: thread (unit w of 32 values d, lane) sums over the waves
+    float* so = reinterpret_cast<float*>(lds);         // [wave][DB][16][64]
+    float* sm = so + NW * DB * 16 * 64;                // [wave][32] m, then [wave][32] l
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) so[((wave * DB + d) * 16 + r) * 64 + lane] = o[d][r];
+    if (half == 0) {
+      sm[wave * 32 + r32] = m;
+      sm[NW * 32 + wave * 32 + r32] = l;
+    }
+    __syncthreads();
+    if (u.row0 + r32 < u.rows) {
+      float top = sm[r32], sum = 0.f, f[NW];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w * 32 + r32]);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        f[w] = fast_exp2(sm[w * 32 + r32] - top);
+        sum += f[w] * sm[NW * 32 + w * 32 + r32];
+      }
+      for (int d = wave; d < DB; d += NW) {
+        f32x16 x;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          x[r] = 0.f;
+#pragma unroll
+          for (int w = 0; w < NW; ++w) x[r] += f[w] * so[((w * DB + d) * 16 + r) * 64 + lane];
+        }
+        emit(token, head, d, x, top, sum);
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -1194,17 +1194,17 @@ template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int s
   } else {
     constexpr int NW = D * sizeof(T) > 256 ? 2 : 4;
     const long long slots = rows / 32 + p.seqs.n;
+    DN_CHECK(slots * (64 * NW) < (1ll << 32), "dn_op_attention_packed: too many rows for one launch");
     hipLaunchKernelGGL((packed_narrow_kernel<T, D, NW, R, false>), dim3((unsigned)slots, p.kv_heads), dim3(64 * NW), 0, s, p, (int)group, 0, part);
   }
   DN_HIP(hipGetLastError());
 }
 
-template <typename T, int D, int NW> void launch(const PackedAttnParams& p, hipStream_t s) {
-  constexpr int BM = 32 * NW;
+template <int D> void launch_f32(const PackedAttnParams& p, hipStream_t s) {
   const int group = p.heads / p.kv_heads;
-  const long long slots = p.T * group / BM + p.seqs.n;
-  DN_CHECK(slots * (64 * NW) < (1ll << 32), "dn_op_attention_packed: too many rows for one launch");
-  hipLaunchKernelGGL((packed_kernel<T, D, NW>), dim3((unsigned)slots, p.kv_heads), dim3(64 * NW), 0, s, p, group);
+  const long long slots = p.T * group / 128 + p.seqs.n;
+  DN_CHECK(slots * 256 < (1ll << 32), "dn_op_attention_packed: too many rows for one launch");
+  hipLaunchKernelGGL((packed_f32_kernel<D>), dim3((unsigned)slots, p.kv_heads), dim3(256), 0, s, p, group);
   DN_HIP(hipGetLastError());
 }
 
@@ -1248,7 +1248,7 @@ template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) 
   const Plan r = plan(sizeof(T), D, p.T, p.heads, p.kv_heads, p.seqs.n, p.max_kv);
   if (r.narrow) return launch_narrow<T, D>(p, r.shares, s);
   if constexpr (sizeof(T) == 4) {
-    launch<T, D, 4>(p, s);
+    launch_f32<D>(p, s);
   } else if constexpr (D == 128) {
     r.waves == 8 ? launch_pipe<D, 64, 8, 4, 2>(p, s) : r.waves == 4 ? launch_pipe<D, 32, 4, 5, 2>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
   } else if constexpr (D == 96) {  // (six waves: whole loads)

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
       if (s < 0) continue;
       const int q0 = p.seqs.q_start[s], q1 = p.seqs.q_start[s + 1], len = p.seqs.kv_len[s];
       const long long k0 = p.seqs.kv_start[s];
-      if (q0 < 0 || t >= q1 || q1 > p.T || len < q1 - q0 || k0 < 0 || k0 > p.kv_rows - len) continue;
+      if (q0 < 0 || t < q0 || t >= q1 || q1 > p.T || len < q1 - q0 || k0 < 0 || k0 > p.kv_rows - len) continue;
       row = k0 + len - (q1 - t);
     }
     raw xa[HC], xb[HC];

@@ -227,6 +227,21 @@ def test_sequences_outside_the_tensors_are_skipped(q_start, kv_start, kv_len, ba
     assert (qo[4 * bad:4 * bad + 4] == 7).all() and all((qo[4 * s:4 * s + 4] != 7).any() for s in good)
 
 
+@pytest.mark.parametrize("q_start", [[4, 0, 8, 2], [12, 3, 1, 0], [0, 9, 5, 12], [2 ** 31 - 1, -5, 7, 2 ** 31 - 1]])
+def test_starts_out_of_order_stay_in_bounds(q_start):
+    """Not a promised input: nothing outside the tensors is read or written (poison around the outputs stays)."""
+    n = 12
+    for kv_len, bound in (([4, 4, 4], 40), ([40, 12, 6], 4000)):
+        seqs = dn.Sequences(int_t(q_start), int_t([0, 10, 20], torch.int64), int_t(kv_len), bound)
+        q, kv = torch.randn(n, 4, 64, device=DEV, dtype=torch.bfloat16), torch.randn(60, 2, 64, device=DEV, dtype=torch.bfloat16)
+        whole, cache = torch.full((n + 200, 4, 64), 7.0, device=DEV, dtype=q.dtype), torch.full((460, 2, 64), 7.0, device=DEV, dtype=q.dtype)
+        o, kc = whole[100:100 + n], cache[200:260]
+        dn.op_attention_packed(q, kv, kv, o, seqs, ws=workspace(q, kv, seqs))
+        pos, gain = torch.zeros(n, 1, device=DEV, dtype=torch.int32), torch.ones(64, device=DEV)
+        dn.op_qk_norm_rope(q, kv[:n], gain, gain, 1e-6, pos, dn.rope_table((64,)), o, kc, seqs=seqs)
+        assert (whole[:100] == 7).all() and (whole[100 + n:] == 7).all() and (cache[:200] == 7).all() and (cache[260:] == 7).all()
+
+
 # ----------------------------------------------------------------------------- attention
 
 def workspace(q, k, seqs):
