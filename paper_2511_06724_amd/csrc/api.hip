@@ -906,12 +906,13 @@ dn_status dn_op_attention_packed(int32_t dtype, const void* q, int64_t ldq, cons
     DN_CHECK(kv_rows >= 1 && kv_rows <= (1ll << 40), "dn_op_attention_packed: bad kv_rows");
     DN_CHECK(seqs, "dn_op_attention_packed: null sequences");
     DN_CHECK(causal == 0 || causal == 1, "dn_op_attention_packed: causal is 0 or 1");
-    DN_CHECK(std::isfinite(scale), "dn_op_attention_packed: the scale must be finite");
+    DN_CHECK(std::fabs(scale) <= 1e38f, "dn_op_attention_packed: the scale's magnitude is at most 1e38");
     const int64_t wq = (int64_t)heads * head_dim, wk = (int64_t)kv_heads * head_dim;
     check_heads(who, dtype, q, ldq, wq);
     check_heads(who, dtype, k, ldk, wk);
     check_heads(who, dtype, v, ldv, wk);
     check_heads(who, dtype, o, ldo, wq);
+    DN_CHECK(o != q && o != k && o != v, "dn_op_attention_packed: the output is not written in place");
     dn::PackedAttnParams p;
     p.seqs = sequences(who, seqs);
     p.q = q, p.k = k, p.v = v, p.o = o;

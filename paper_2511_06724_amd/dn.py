@@ -9,6 +9,7 @@ module raises if the library has not been built: there is no fallback.
 import ctypes as C
 import functools
 import os
+import struct
 
 import numpy as np
 
@@ -79,11 +80,6 @@ class _Sequences(C.Structure):
                 ("kv_len", C.c_void_p)]
 
 
-class _Rotation(C.Structure):
-    _fields_ = [("table", C.c_void_p), ("pos", C.c_void_p), ("n_axes", C.c_int32), ("rot_dim", C.c_int32),
-                ("pairing", C.c_int32)]
-
-
 def _load():
     # One HIP runtime per process: PyTorch bundles its own libamdhip64 with the
     # same soname as ROCm's. Importing torch first makes the library bind to that
@@ -115,8 +111,8 @@ def _load():
         "ac_mx_lookup_bytes": [I32, I64, I32, C.POINTER(I64)],
         "ac_mx_lookup": [I32, P, I32, P, I64, I32, C.POINTER(_KTable), P, P, P, P, P],
         "dn_rope_table": [P, P, I32, P, P],
-        "dn_op_rope": [I32, P, I64, P, I64, I64, I32, I32, C.POINTER(_Rotation), P],
-        "dn_op_qk_norm_rope": [I32, P, I64, P, I64, P, I64, I64, I32, I32, I32, P, P, F32, C.POINTER(_Rotation),
+        "dn_op_rope": [I32, P, I64, P, I64, I64, I32, I32, P, P],
+        "dn_op_qk_norm_rope": [I32, P, I64, P, I64, P, I64, I64, I32, I32, I32, P, P, F32, P,
                                C.POINTER(_Sequences), P, I64, P, I64, P, I64, I64, P],
         "dn_attention_packed_bytes": [I32, I64, I32, I32, I32, I32, I32, C.POINTER(I64)],
         "dn_op_attention_packed": [I32, P, I64, P, I64, P, I64, P, I64, I64, I64, I32, I32, I32, C.POINTER(_Sequences), I32,
@@ -187,6 +183,19 @@ def _stream(stream):
     if stream is None:
         return _raw_stream()()
     return getattr(stream, "cuda_stream", stream)
+
+
+@functools.lru_cache(maxsize=None)
+def _current_device():
+    import torch
+    return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _stream_on(device, stream, name):
+    """The stream of a call whose tensors all lie on GPU device (-1: they do not)."""
+    if device < 0 or device != _current_device()():
+        raise ValueError(f"{name}: all tensors must lie on the current GPU")
+    return _stream(stream)
 
 
 def to_c_config(cfg: DnConfig) -> _Config:
@@ -595,6 +604,9 @@ class Sequences:
         _dense(kv_start, torch.int64, (n,), "Sequences: kv_start")
         _dense(q_start, torch.int32, (n + 1,), "Sequences: q_start")
         self.n, self.max_kv_len = n, int(max_kv_len)
+        self.device = kv_len.get_device()
+        if not self.device == kv_start.get_device() == q_start.get_device():
+            raise ValueError("Sequences: tensors of one device are needed")
         self._keep = (q_start, kv_start, kv_len)
         self._c = _Sequences(n, self.max_kv_len, _ptr(q_start), _ptr(kv_start), _ptr(kv_len))
         self.ref = C.byref(self._c)
@@ -622,8 +634,9 @@ class RopeTable:
             raise ValueError("rope_table: one frequency per rotated pair is needed")
         self.rot_dim, self.n_axes = sum(self.axis_dims), len(self.axis_dims)
         self.data = torch.empty(DN_ROPE_TABLE_BYTES, device=device, dtype=torch.uint8)
-        self.address = self.data.data_ptr()
-        _check(lib.dn_rope_table(f.ctypes.data, dims.ctypes.data, self.n_axes, self.address, _stream(stream)))
+        self.address, self.device = self.data.data_ptr(), self.data.get_device()
+        _check(lib.dn_rope_table(f.ctypes.data, dims.ctypes.data, self.n_axes, self.address,
+                                 _stream_on(self.device, stream, "rope_table")))
 
 
 def rope_table(axis_dims, theta=10000.0, per_axis=True, freqs=None, device="cuda", stream=None):
@@ -632,9 +645,13 @@ def rope_table(axis_dims, theta=10000.0, per_axis=True, freqs=None, device="cuda
     return RopeTable(axis_dims, rope_freqs(axis_dims, theta, per_axis) if freqs is None else freqs, device, stream)
 
 
+# dn_rotation as bytes: a fifth of the time that a ctypes structure takes, in a call of 5 us
+_rotation_bytes = struct.Struct("@PPiii4x").pack
+
+
 def _rotation(table, pos, rows, pairing, name):
-    return C.byref(_Rotation(table.address, _dense(pos, _plain_types()[0], (rows, table.n_axes), f"{name}: pos"), table.n_axes,
-                             table.rot_dim, pairing))
+    return _rotation_bytes(table.address, _dense(pos, _plain_types()[0], (rows, table.n_axes), f"{name}: pos"), table.n_axes,
+                           table.rot_dim, pairing)
 
 
 def op_rope(x, pos, table, y=None, pairing=DN_ROPE_PAIRS, stream=None):
@@ -647,8 +664,10 @@ def op_rope(x, pos, table, y=None, pairing=DN_ROPE_PAIRS, stream=None):
     if yt != dt or y_shape != shape:
         raise ValueError("op_rope: y must have the type and shape of x")
     rows, heads, dim = shape
-    _check(lib.dn_op_rope(dt, src, ldx, dst, ldy, rows, heads, dim, _rotation(table, pos, rows, pairing, "op_rope"),
-                          _stream(stream)))
+    turn = _rotation(table, pos, rows, pairing, "op_rope")
+    dev = x.get_device()
+    on = _stream_on(dev if dev == y.get_device() == pos.get_device() == table.device else -1, stream, "op_rope")
+    _check(lib.dn_op_rope(dt, src, ldx, dst, ldy, rows, heads, dim, turn, on))
     return y
 
 
@@ -676,11 +695,16 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, eps, pos, table, q_out, k_out, v=None,
         if vt != dt or vot != dt or v_shape != k_shape or vo_shape != ko_shape:
             raise ValueError(f"{name}: values must have the type and shape of the keys, and so must their output")
     f32 = _plain_types()[1]
-    _check(lib.dn_op_qk_norm_rope(dt, pq, ldq, pk, ldk, pv, ldv, rows, heads, k_shape[1], dim,
-                                  _dense(q_gain, f32, (dim,), "op_qk_norm_rope: q_gain"),
-                                  _dense(k_gain, f32, (dim,), "op_qk_norm_rope: k_gain"), eps,
-                                  _rotation(table, pos, rows, pairing, name), None if seqs is None else seqs.ref, pqo, ldqo, pko,
-                                  ldko, pvo, ldvo, ko_shape[0], _stream(stream)))
+    pqg = _dense(q_gain, f32, (dim,), "op_qk_norm_rope: q_gain")
+    pkg = _dense(k_gain, f32, (dim,), "op_qk_norm_rope: k_gain")
+    turn = _rotation(table, pos, rows, pairing, name)
+    dev = q.get_device()
+    one = (dev == k.get_device() == q_out.get_device() == k_out.get_device() == q_gain.get_device() == k_gain.get_device()
+           == pos.get_device() == table.device and (v is None or dev == v.get_device() == v_out.get_device())
+           and (seqs is None or dev == seqs.device))
+    on = _stream_on(dev if one else -1, stream, name)
+    _check(lib.dn_op_qk_norm_rope(dt, pq, ldq, pk, ldk, pv, ldv, rows, heads, k_shape[1], dim, pqg, pkg, eps, turn,
+                                  None if seqs is None else seqs.ref, pqo, ldqo, pko, ldko, pvo, ldvo, ko_shape[0], on))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -711,9 +735,12 @@ def op_attention_packed(q, k, v, o, seqs, causal=True, scale=None, ws=None, stre
     need = _attention_packed_bytes(dt, rows, heads, kv_heads, dim, seqs.n, seqs.max_kv_len)
     if ws is not None:
         _buffer(ws, need, name)
+    dev = q.get_device()
+    one = dev == k.get_device() == v.get_device() == o.get_device() == seqs.device and (ws is None or dev == ws.get_device())
+    on = _stream_on(dev if one else -1, stream, name)
     _check(lib.dn_op_attention_packed(dt, pq, ldq, pk, ldk, pv, ldv, po, ldo, rows, kv_rows, heads, kv_heads, dim, seqs.ref,
                                       1 if causal else 0, dim ** -0.5 if scale is None else scale,
-                                      ws.data_ptr() if need and ws is not None else None, _stream(stream)))
+                                      ws.data_ptr() if need and ws is not None else None, on))
 
 
 def packed_weight_elems(dtype, N, K):

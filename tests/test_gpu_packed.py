@@ -428,6 +428,61 @@ def test_extreme_scores():
     assert torch.allclose(b.o[:4], b.v[a:a + 70].mean(0).expand(4, 1, 64), atol=1e-5)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("longest,q_max", [(150, 1), (3000, 1), (900, 6), (400, 130)])
+def test_many_sequences(dtype, longest, q_max):
+    """More sequences than a wave has lanes, among them empty ones."""
+    rng = np.random.default_rng(longest)
+    q_len = [int(n) for n in rng.integers(0, q_max + 1, 211)]
+    kv_len = [n + int(m) for n, m in zip(q_len, rng.integers(0, longest - q_max, 211))]
+    b = Batch(q_len, kv_len, 4, 2, 64, dtype, seed=5)
+    b.run(True)
+    b.check(True, rows=np.array([0, 1, 5, 31, 32, 70, 129]))
+
+
+def test_a_shared_prefix():
+    """Sequences whose keys overlap: all of them begin with the same rows."""
+    for dtype in TYPES:
+        b = Batch([1] * 5 + [40], [1200, 1100, 700, 1, 1200, 1199], 8, 2, 128, dtype)
+        b.start = [b.start[0]] * 6
+        b.seqs = dn.Sequences(int_t(b.qs), int_t(b.start, torch.int64), int_t(b.kv_len), 1200)
+        b.run(True)
+        b.check(True, rows=np.arange(0, 40, 13))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_offsets_past_32_bits(dtype):
+    """Keys and values that lie 4 GiB and more behind the tensors' starts, inside one sequence and at its start."""
+    rng, hk, dim, width = np.random.default_rng(2), 2, 64, 1024
+    rows = 2 ** 32 // (width * dim * (2 if dtype == dn.DN_BF16 else 4)) + 4000
+    kv = torch.empty(rows, width, dim, device=DEV, dtype=tdtype(dtype))
+    k, v = kv[:, :hk], kv[:, hk:2 * hk]
+    kv[:, :2 * hk].normal_(generator=torch.Generator(device=DEV).manual_seed(3))
+    tail = rows - 1500
+    kh, vh = host(k.contiguous()), host(v.contiguous())
+    for q_len, kv_len, start in (([1, 1], [rows, 1500], [0, tail]), ([2000, 300], [rows, 1500], [0, tail])):
+        q, qv = heads(rng, sum(q_len), 4, dim, dtype)
+        o = torch.empty_like(q)
+        seqs = dn.Sequences(int_t(np.cumsum([0] + q_len)), int_t(start, torch.int64), int_t(kv_len), rows)
+        dn.op_attention_packed(q, k, v, o, seqs, causal=False, ws=workspace(q, k, seqs))
+        got, up = host(o), U[dtype] if dtype == dn.DN_BF16 else 0.0
+        for s in range(2):
+            for i in {0, q_len[s] - 1}:
+                at, a, m = i + s * q_len[0], start[s], kv_len[s]
+                ref, mass = P.attention(qv[at:at + 1], kh[a:a + m], vh[a:a + m], False, dim ** -0.5)
+                d = (dim + 4) * W * np.abs(qv[at]).sum(-1).max() * np.abs(kh).max() * dim ** -0.5 + 2 * W
+                close(got[at:at + 1], ref, (2 * (d + up) + (m + 4) * W) * mass + U[dtype] * np.abs(ref))
+    # the last rows of the cache are written
+    x, gain = heads(rng, 3, hk, dim, dtype)[0], torch.ones(dim, device=DEV)
+    seqs = dn.Sequences(int_t([0, 3]), int_t([tail], torch.int64), int_t([1500]), rows)
+    near = (torch.empty(3, hk, dim, device=DEV, dtype=x.dtype) for _ in range(2))
+    args = (x, x, gain, gain, 1e-6, int_t([[5], [6], [7]]), dn.rope_table((dim,)))
+    qo, ko = near
+    dn.op_qk_norm_rope(*args, qo, k, x, v, seqs)
+    dn.op_qk_norm_rope(*args, qo, ko)
+    assert torch.equal(k[-3:], ko) and torch.equal(v[-3:], x)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.0])
 def test_scales(scale):
     for dtype in TYPES:
@@ -465,6 +520,58 @@ def test_a_captured_call_follows_lengths_and_data():
         replayed = b.o.clone()
         b.ws.fill_(0xff)
         assert torch.equal(b.run(True), replayed)
+
+
+def test_a_captured_step_generates():
+    """Norm, rotation into the cache and attention of one token per request, captured together with the work that moves
+    positions and lengths on: replayed, with eager calls between, it gives the eager steps' bits."""
+    hq, hk, dim, cap = 4, 2, 64, 700
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    new = [torch.empty(3, hq + 2 * hk, dim, device=DEV, dtype=torch.bfloat16).normal_(generator=gen) for _ in range(4)]
+    table, gain = dn.rope_table((dim,)), torch.ones(dim, device=DEV)
+
+    def state():
+        kv_len = int_t([600, 0, 33])
+        seqs = dn.Sequences(int_t([0, 1, 2, 3]), int_t([0, cap, 2 * cap], torch.int64), kv_len, cap)
+        kc, vc = (torch.zeros(3 * cap, hk, dim, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+        kc.normal_(generator=torch.Generator(device=DEV).manual_seed(6))
+        vc.normal_(generator=torch.Generator(device=DEV).manual_seed(7))
+        x = torch.empty_like(new[0])
+        q, o = (torch.empty(3, hq, dim, device=DEV, dtype=x.dtype) for _ in range(2))
+        return dict(kv_len=kv_len, seqs=seqs, kc=kc, vc=vc, x=x, q=q, o=o, pos=int_t([[599], [-1], [32]]), ws=workspace(q, kc, seqs))
+
+    def step(s):
+        s["kv_len"].add_(1)
+        s["pos"].add_(1)
+        x = s["x"]
+        dn.op_qk_norm_rope(x[:, :hq], x[:, hq:hq + hk], gain, gain, 1e-6, s["pos"], table, s["q"], s["kc"], x[:, hq + hk:], s["vc"], s["seqs"])
+        dn.op_attention_packed(s["q"], s["kc"], s["vc"], s["o"], s["seqs"], ws=s["ws"])
+
+    a, b = state(), state()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step(state())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step(b)
+    for x in new:
+        a["x"].copy_(x)
+        b["x"].copy_(x)
+        step(a)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a["o"], b["o"]) and torch.equal(a["kc"], b["kc"]) and torch.equal(a["vc"], b["vc"])
+        assert torch.equal(a["kv_len"], b["kv_len"]) and torch.isfinite(a["o"]).all() and (a["o"] != 0).any()
+
+
+def test_tensors_of_another_device_are_refused():
+    b = Batch([1], [9], 2, 2, 64, dn.DN_BF16)
+    with pytest.raises(ValueError, match="current GPU"):
+        dn.op_attention_packed(b.q, b.k.cpu(), b.v, b.o, b.seqs)
+    with pytest.raises(ValueError, match="current GPU"):
+        dn.op_rope(b.q, torch.zeros(len(b.q), 1, dtype=torch.int32), dn.rope_table((64,)))
 
 
 def test_two_streams_at_once():

@@ -18,7 +18,7 @@ def seqs(**change):
 
 def rot(**change):
     a = {**dict(table=P, pos=P, n_axes=2, rot_dim=64, pairing=0), **change}
-    return C.byref(dn._Rotation(a["table"], a["pos"], a["n_axes"], a["rot_dim"], a["pairing"]))
+    return dn._rotation_bytes(a["table"] or 0, a["pos"] or 0, a["n_axes"], a["rot_dim"], a["pairing"])
 
 
 BAD_SEQS = [dict(n=0), dict(n=-1), dict(max_kv_len=0), dict(q_start=None), dict(kv_start=None), dict(kv_len=None), dict(q_start=P + 2),
@@ -72,7 +72,7 @@ def test_qk_norm_rope_refused(change):
                                      a["vo"], a["ldvo"], a["rows"], None) == dn.DN_EINVAL
 
 
-ATTN = dict(dtype=dn.DN_BF16, q=P, ldq=256, k=P, ldk=128, v=P, ldv=128, o=P, ldo=256, T=4, rows=100, heads=4, kv_heads=2, dim=64, seqs=seqs(),
+ATTN = dict(dtype=dn.DN_BF16, q=P, ldq=256, k=P, ldk=128, v=P, ldv=128, o=P + 64, ldo=256, T=4, rows=100, heads=4, kv_heads=2, dim=64, seqs=seqs(),
             causal=1, scale=0.125, ws=P)
 
 
@@ -80,7 +80,8 @@ ATTN = dict(dtype=dn.DN_BF16, q=P, ldq=256, k=P, ldk=128, v=P, ldv=128, o=P, ldo
                                     dict(ldq=248), dict(ldk=64), dict(ldv=124), dict(ldo=0), dict(T=0), dict(T=2 ** 31), dict(T=2 ** 30),
                                     dict(rows=0), dict(rows=2 ** 41), dict(heads=0), dict(heads=5), dict(kv_heads=0), dict(kv_heads=3),
                                     dict(dim=48), dict(dim=256, ldq=1024, ldk=512, ldv=512, ldo=1024), dict(seqs=None), dict(causal=2),
-                                    dict(scale=float("nan")), dict(scale=float("inf")), dict(ws=P + 8)] + [dict(seqs=seqs(**b)) for b in BAD_SEQS])
+                                    dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-3e38),
+                                    dict(o=P), dict(ws=P + 8)] + [dict(seqs=seqs(**b)) for b in BAD_SEQS])
 def test_attention_packed_refused(change):
     a = {**ATTN, **change}
     assert dn.lib.dn_op_attention_packed(a["dtype"], a["q"], a["ldq"], a["k"], a["ldk"], a["v"], a["ldv"], a["o"], a["ldo"], a["T"], a["rows"],
@@ -127,6 +128,19 @@ def test_binding_refuses_positions_and_gains():
                    dict(q_out=t(5, 4, 64, dtype=torch.float32)), dict(v=t(5, 2, 64)), dict(v=t(5, 4, 64), v_out=t(5, 2, 64))):
         with pytest.raises(ValueError):
             dn.op_qk_norm_rope(**{**good, **change}, eps=1e-6, pos=pos, table=Table, stream=0)
+
+
+def test_binding_refuses_host_tensors():
+    class Table:
+        n_axes, rot_dim, address, device = 2, 64, P, -1
+    i32 = torch.int32
+    s = dn.Sequences(t(3, dtype=i32), t(2, dtype=torch.int64), t(2, dtype=i32), 9)
+    q, k, pos, g = t(5, 4, 64), t(9, 2, 64), t(5, 2, dtype=i32), t(64, dtype=torch.float32)
+    for call in (lambda: dn.op_rope(q, pos, Table, stream=0), lambda: dn.op_attention_packed(q, k, k, q, s, stream=0),
+                 lambda: dn.op_qk_norm_rope(q, k[:5], g, g, 1e-6, pos, Table, q, k, k[:5], k, s, stream=0),
+                 lambda: dn.rope_table((32, 32), device="cpu", stream=0)):
+        with pytest.raises(ValueError, match="current GPU"):
+            call()
 
 
 def test_default_frequencies():
