@@ -1063,26 +1063,41 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D * siz
 template <int D> struct JoinedRow {
   static constexpr int E = (D + 63) / 64;
   float top = kLowest, sum = 0.f, v[E] = {};
-  __device__ __forceinline__ void add(const Partials& part, int w0, int n, int r, int first, int step) {
+  // (with loads of W parts side by side)
+  template <int W> __device__ __forceinline__ void add(const Partials& part, int w0, int n, int r, int first, int step) {
     const int lane = threadIdx.x & 63;
     auto at = [&](int k) { return (2ll * (w0 + k) + (k == 0 ? 1 : 0)) * 32 + r; };
     for (int c = first; c < n; c += 64 * step) {
-      const int mine = c + lane * step;
+      const int mine = c + lane * step, cnt = min(64, (n - c + step - 1) / step);
       const float2 ml = mine < n ? part.ml[at(mine)] : make_float2(kLowest, 0.f);
+      // values and statistics come from another XCD's writes: one wait for both
+      float x[W][E];
+      auto load = [&](int k0) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          const float* o = part.o + at(c + min(k0 + j, cnt - 1) * step) * D;
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[j][e] = o[min(e * 64 + lane, D - 1)];
+        }
+      };
+      load(0);
       const float up = fmaxf(top, wave_max(ml.x)), alpha = fast_exp2(top - up);
       top = up;
       sum *= alpha;
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] *= alpha;
       const float f = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top), fl = f * ml.y;
-      const int cnt = min(64, (n - c + step - 1) / step);
-#pragma unroll 8
-      for (int k = 0; k < cnt; ++k) {
-        const float fk = __shfl(f, k, 64);
-        sum += __shfl(fl, k, 64);
-        const float* o = part.o + at(c + k * step) * D;
+      for (int k0 = 0; k0 < cnt; k0 += W) {
+        if (k0) load(k0);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] += fk * o[min(e * 64 + lane, D - 1)];  // (without a branch: loads side by side)
+        for (int j = 0; j < W; ++j) {
+          if (k0 + j < cnt) {
+            const float fk = __shfl(f, k0 + j, 64);
+            sum += __shfl(fl, k0 + j, 64);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] += fk * x[j][e];
+          }
+        }
       }
     }
   }
@@ -1096,18 +1111,24 @@ template <int D> struct JoinedRow {
   }
 };
 
-// Joins units of few parts: four waves take the rows of the units that four shares begin in turn.
+// Joins units of few parts: four waves (of each of gridDim.y workgroups) take the rows of the units that four shares begin in turn.
 template <typename T, int D> __global__ __launch_bounds__(256) void join_rows_kernel(PackedAttnParams p, int group, int shares, Partials part) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = 4 * gridDim.y, wave = __builtin_amdgcn_readfirstlane(4 * blockIdx.y + (threadIdx.x >> 6));
+  DividedUnit units[4];  // (loads side by side)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) units[i] = part.unit[min((int)blockIdx.x * 4 + i, shares - 1)];
   int before = 0;
-  for (int w0 = blockIdx.x * 4; w0 < min(shares, (int)blockIdx.x * 4 + 4); ++w0) {
-    const DividedUnit u = part.unit[w0];
-    for (int r = (wave - before) & 3; r < u.rows; r += 4) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const DividedUnit u = units[i];
+    const int w0 = blockIdx.x * 4 + i;
+    if (w0 >= shares) return;
+    for (int r = (wave + waves - before) % waves; r < u.rows; r += waves) {
       JoinedRow<D> row;
-      row.add(part, w0, u.last - w0 + 1, r, 0, 1);
+      row.template add<16>(part, w0, u.last - w0 + 1, r, 0, 1);
       row.template store<T>(p, group, u, r);
     }
-    before += u.rows;
+    before = (before + u.rows) % waves;
   }
 }
 
@@ -1121,7 +1142,7 @@ template <typename T, int D> __global__ __launch_bounds__(64 * kJoin) void join_
   const DividedUnit u = part.unit[w0];
   for (int r = blockIdx.y; r < u.rows; r += gridDim.y) {
     JoinedRow<D> row;
-    row.add(part, w0, u.last - w0 + 1, r, wave, kJoin);
+    row.template add<4>(part, w0, u.last - w0 + 1, r, wave, kJoin);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < E; ++e) s_v[wave][e * 64 + lane] = row.v[e];
@@ -1165,10 +1186,12 @@ size_t partials(void* ws, int D, int shares, Partials& r) {
 // 128: 181 us, with two waves and 512 200, with four and 256 212. Others: four waves on a unit.
 constexpr int most_shares(int row_bytes) { return row_bytes <= 64 ? 2048 : 1024; }
 
-// Of few blocks the shares are fewer: a block takes a wave about 1 us (fp32 2.5) and a part takes the join about 0.04 us.
-// s shares of B blocks, of which the largest unit has `most`, take t B / s + 0.04 s most / B.
+// Of few blocks the shares are fewer: with a block's time t and a part's time in the join c, s shares of B blocks, of which the
+// largest unit has `most`, take t B / s + c s most / B, least at s = sqrt(t / c) B / sqrt(most). The root is 5 for bf16 and 12
+// for fp32, by measurement (fp32, one context of 3483 keys: 18.5 us with 8, 15.7 with 12 or 16; bf16, six contexts up to
+// 48 k, 4/1 x 32: 22.0 with 5, 23.1 with 7.5, 26.2 with 10).
 int shares_of(long long blocks, long long most, long long units, int elem, int D) {
-  const double s = (elem == 2 ? 5.0 : 8.0) * blocks / std::sqrt((double)most);
+  const double s = (elem == 2 ? 5.0 : 12.0) * blocks / std::sqrt((double)most);
   return (int)std::min<long long>({std::max((long long)std::min(s, 1e9), units), blocks, most_shares(D * elem)});
 }
 
@@ -1185,12 +1208,16 @@ template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int s
     hipLaunchKernelGGL((packed_narrow_kernel<T, D, 1, R, true>), dim3(shares), dim3(64), 0, s, p, (int)group, shares, part);
     DN_HIP(hipGetLastError());
     const long long per = std::min<long long>(32, (rows + p.seqs.n - 1) / p.seqs.n);  // rows of a unit, in the mean
+    const long long units = (rows / 32 + p.seqs.n) * p.kv_heads;
     // up to about 32 parts of the largest unit, and not so few rows that every one can have a workgroup (16/2 x 128, 128 tokens
-    // behind 16 k keys: 98 us, with a workgroup per row 128; 13 single tokens, 1/1 x 96: 14.8 and 10.4)
-    if (shares * per > 1024 && shares * most <= 32 * blocks)
-      hipLaunchKernelGGL((join_rows_kernel<T, D>), dim3((shares + 3) / 4), dim3(256), 0, s, p, (int)group, shares, part);
-    else
+    // behind 16 k keys: 71 us, with a workgroup per row 128; 13 single tokens, 1/1 x 96: 14.8 and 10.4). The rows of few
+    // units go over several workgroups, a row or so a wave (the former: 98 with one)
+    if (shares * per > 1024 && shares * most <= 32 * blocks) {
+      const unsigned split = (unsigned)std::max<long long>(1, std::min(per / 4, 1024 / units));
+      hipLaunchKernelGGL((join_rows_kernel<T, D>), dim3((shares + 3) / 4, split), dim3(256), 0, s, p, (int)group, shares, part);
+    } else {
       hipLaunchKernelGGL((join_kernel<T, D>), dim3(shares, (unsigned)per), dim3(64 * kJoin), 0, s, p, (int)group, part);
+    }
   } else {
     constexpr int NW = D * sizeof(T) > 256 ? 2 : 4;
     const long long slots = rows / 32 + p.seqs.n;
@@ -1223,10 +1250,15 @@ struct Plan {
 };
 // Measured, us (heads/kv_heads x head dim):
 //  - few rows a sequence: narrow. Up to 256 keys a unit is one workgroup's (77 keys, 20/20 x 64: 6.1); longer ones are divided.
-//  - too few tiles to fill the CUs and long keys: narrow, divided (16/2 x 128, 128 tokens behind 16 k keys: 129, tiles 275;
-//    32/8 x 128, 8 x 16 behind 8 k: 126, 213; but 4 x 64 tokens: 168, tiles 143: the parts of more rows cost more).
+//  - too few tiles to fill the CUs and long keys: narrow, divided. A tile's time goes with the keys (0.017 us each of 128
+//    wide heads), a divided call's with keys and tiles behind about 20 us, so the most tiles that are divided fall from 112
+//    as the keys get fewer (16/2 x 128, 128 tokens behind 16 k keys: 71, tiles 273; 32/8 x 128, 4 x 64 behind 8 k: 125, 143;
+//    16/4 x 128, 8 x 32 behind 2 k: 33.6, 41.4; but 8/8 x 64, 4 x 50 behind 700: 47, tiles 12.8; 2 x 300 behind 700: 27, 14.4).
+//    Many units that read the same keys gain less: 64 (12/3 x 128, 662 of 2253: 57.6, tiles 44.6; 1/1, 3000: 36.2, 56.4).
 //  - fp32, bound by the matrix cores either way: narrow while its smaller units fill more CUs (10/2 x 64, 7 chunks behind up
-//    to 825 keys: 23.6, tiles 64.8; 12/12 x 64, 16 x 77 tokens: 21.0, 26.0; 10/10 x 64, 2 x 1024 tokens: 87, tiles 82.6).
+//    to 825 keys: 24.7, tiles 64.8; 12/12 x 64, 16 x 77 tokens: 21.0, 26.0; 10/10 x 64, 2 x 1024 tokens: 87, tiles 79).
+//    Divided past 256 keys of wide heads, whose units have two waves by their LDS (8/2 x 128, 4 x 20 behind 500: 19.5, else
+//    44.7), and past 1024 of others, with four (16/4 x 64, 8 x 10 behind 900: 25.8, else 29.0; 8/8 x 64, 500 of 1000: 22.4, 17.8).
 //  - tiles: 8 waves of 32 rows where there are tiles for every CU and the border is small beside them (20/20 x 128, two
 //    images of 4173 tokens: 357, 4 waves 402; 8 x 512 tokens: 40.0, 36.3); 2 waves for short prompts (20/20 x 64,
 //    64 of 49 tokens in the mean: 18.1, 4 waves 20.6, 8 waves 39.2); else 4 (64 wide: 2 x 10/10, 4096 tokens: 120, 8 waves 141).
@@ -1235,9 +1267,9 @@ Plan plan(int elem, int D, long long T, int heads, int kv_heads, int n, int max_
   auto tiles = [&](int bm) { return (rows / bm + n) * kv_heads; };
   const bool few = rows <= 32ll * n, some = rows < 96ll * n;
   Plan r;
-  r.narrow = few || (elem == 4 ? some || tiles(128) < 128 : max_kv > 512 && tiles(128) < (some ? 120 : 40));
+  r.narrow = few || (elem == 4 ? some || tiles(128) < 128 : tiles(128) <= (rows < 1024ll * n ? 112 : 64) - 100000 / max_kv);
   if (r.narrow) {
-    if (max_kv > (few || elem == 2 ? 256 : 1024)) r.shares = (int)std::min<long long>(most_shares(D * elem), units * ((max_kv + 31ll) / 32));
+    if (max_kv > (few || elem == 2 || D > 64 ? 256 : 1024)) r.shares = (int)std::min<long long>(most_shares(D * elem), units * ((max_kv + 31ll) / 32));
   } else {
     r.waves = some ? 2 : D == 128 && rows >= 1024ll * n && tiles(256) >= 256 ? 8 : 4;
   }
