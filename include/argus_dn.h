@@ -404,8 +404,8 @@ typedef struct {
  * neighbours (DN_ROPE_PAIRS: values 2i, 2i + 1) or half the rotated width apart (DN_ROPE_HALVES: values i,
  * i + rot_dim / 2; rot_dim % 8 == 0). With several axes (time, height, width) the first axis_dims[0] / 2 pairs
  * turn with axis 0, the next axis_dims[1] / 2 with axis 1, and so on. Positions are any int32; the angle
- * is exact to 2^-31 of a turn at any of them. Negated positions turn back: the inverse,
- * and the gradient. */
+ * is exact to 2^-31 of a turn at any of them and any frequency of dn_rope_table, its sine and cosine to 2^-22.
+ * Negated positions turn back: the inverse, and the gradient. */
 #define DN_ROPE_MAX_AXES 4
 #define DN_ROPE_MAX_DIM 256
 #define DN_ROPE_TABLE_BYTES 2048

@@ -815,10 +815,7 @@ dn_status dn_rope_table(const double* freqs, const int32_t* axis_dims, int32_t n
       for (int j = 0; j < axis_dims[a] / 2; ++j, ++n) {
         DN_CHECK(std::isfinite(freqs[n]) && std::fabs(freqs[n]) <= 65536.0,
                  "dn_rope_table: frequencies must be finite, at most 65536");
-        long double turn = static_cast<long double>(freqs[n]) / 6.283185307179586476925286766559L;
-        turn -= std::floor(turn);
-        const long double f = std::round(std::ldexp(turn, 64));
-        p.turn[n] = f >= 18446744073709551616.0L ? 0 : static_cast<unsigned long long>(f);
+        p.turn[n] = dn::rope_turn(freqs[n]);
         p.axis[n] = static_cast<unsigned char>(a);
       }
     }

@@ -52,6 +52,8 @@ struct RopeTableParams {
   unsigned long long turn[kRopePairs];
   unsigned char axis[kRopePairs];
 };
+// freq radians in turns: the fraction, in units of 2^-64, within one of them (|freq| <= 2^16).
+unsigned long long rope_turn(double freq);
 void rope_table(const RopeTableParams& p, void* table, hipStream_t s);
 
 // Rotates (and, with gains, RMS-normalises first) the heads of packed rows; copies the heads of v.

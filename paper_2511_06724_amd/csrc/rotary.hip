@@ -6,7 +6,7 @@
 // Angles: positions of long contexts times a frequency lose their fraction of a turn in 32 bits (at
 // position 10^6 an fp32 product is off by 0.06 radians). The table holds f_i / 2 pi as a 64-bit
 // binary fraction of a turn; its product with the position modulo 2^64 is the angle modulo one turn
-// exactly (to 2^-64 turns per position), of which the top 32 bits are kept. Sine and cosine of an
+// exactly (to 2^-64 turns per position, at any frequency), of which the top 32 bits are kept. Sine and cosine of an
 // eighth of a turn either way are Taylor polynomials (truncated below 2^-29), so all of an fp32
 // result's error is rounding.
 //
@@ -16,6 +16,7 @@
 // after another, which share the row's angles. 32,760 rows of 20 heads of 128 in fp32 122 us, 20 + 20 in bf16 with their norms
 // 120 us: 5.5 TB/s of reads and writes, where a large copy moves 5.1. Of 80 values a group of 16 lanes uses 10: 3.8 TB/s.
 #include <algorithm>
+#include <cmath>
 
 #include "packed.h"
 
@@ -215,6 +216,22 @@ template <typename T, int G> void launch_kind(const RotaryParams& p, hipStream_t
 }
 
 }  // namespace
+
+// freq = m 2^e with 53 bits of m, times 128 bits of 1 / (2 pi), in integers: the whole turns drop off as bits past the
+// 64th. In 64 bits of a long double they would take the place of the fraction's last bits, and 2 pi's own error grows with the
+// frequency: 2^-21 of a turn at 3 10^4 radians a position and position 2^31, where this is within 2^-32.
+unsigned long long rope_turn(double freq) {
+  typedef unsigned __int128 u128;
+  int e;
+  const unsigned long long m = static_cast<unsigned long long>(std::ldexp(std::frexp(std::fabs(freq), &e), 53));
+  e -= 53;
+  const unsigned long long hi = 0x28be60db9391054aull, lo = 0x7f09d5f47d4d3770ull;  // 2^128 / (2 pi)
+  const u128 top = static_cast<u128>(m) * hi + (static_cast<u128>(m) * lo >> 64);   // m 2^64 / (2 pi)
+  const int drop = -e;  // at least 36 by the bound of freq
+  if (drop >= 128) return 0;
+  const unsigned long long turn = static_cast<unsigned long long>(top >> drop) + static_cast<unsigned long long>(top >> (drop - 1) & 1);
+  return freq < 0 ? 0 - turn : turn;
+}
 
 void rope_table(const RopeTableParams& p, void* table, hipStream_t s) {
   hipLaunchKernelGGL(rope_table_kernel, dim3(1), dim3(kRopePairs), 0, s, p, static_cast<RopeEntry*>(table));

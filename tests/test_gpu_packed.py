@@ -17,6 +17,7 @@ import torch
 from oracle import packed as P
 from paper_2511_06724_amd import dn
 from tests.gpu_util import DEV, announce, host, tdtype
+from tests.test_packed_cpu import turns
 
 pytestmark = pytest.mark.gpu
 
@@ -119,6 +120,20 @@ def test_values_past_the_rotated_width_pass_whole():
         y = dn.op_rope(x, pos, dn.rope_table((32,)), pairing=pairing)
         assert torch.equal(torch.nan_to_num(y[..., 32:], 7.0, 8.0, 9.0), torch.nan_to_num(x[..., 32:], 7.0, 8.0, 9.0))
         assert torch.isfinite(y[..., :32]).all()
+
+
+@pytest.mark.parametrize("freq", [10.0, 100.0, 30000.3, -65536.0])
+def test_rope_at_any_frequency(freq):
+    """The angle of far positions, taken in integers: 2^-31 of a turn moves values of size one by 0.05 w, beside the rotation's
+    own 8 w and the output's rounding."""
+    pos = [2 ** 31 - 1, -2 ** 31, 1234567891, -7, 0]
+    x = torch.zeros(len(pos), 1, 8, device=DEV)
+    x[..., 0] = 1.0
+    y = host(dn.op_rope(x, int_t([[p] for p in pos]), dn.rope_table((2,), freqs=[freq])))[:, 0]
+    angle = [2 * np.pi * (p * turns(freq) % 2 ** 64) / 2.0 ** 64 for p in pos]
+    close(y[:, 0], np.cos(angle), 9.05 * W)
+    close(y[:, 1], np.sin(angle), 9.05 * W)
+    assert not y[:, 2:].any()
 
 
 # ----------------------------------------------------------------------------- norm and rotation

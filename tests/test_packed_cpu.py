@@ -148,3 +148,30 @@ def test_default_frequencies():
     assert np.allclose(dn.rope_freqs((4, 4), 100.0, per_axis=False), 100.0 ** (-np.arange(4) / 4))
     with pytest.raises(ValueError):
         dn.RopeTable((4,), [1.0], "cpu", stream=0)
+
+
+def turns(freq):
+    """freq / (2 pi) modulo 1 in units of 2^-64, rounded, in integers (pi by Machin's formula in 400 bits)."""
+    one = 1 << 400
+
+    def arctan_of_inverse(x):
+        total, term, n = 0, one // x, 1
+        while term:
+            total += term // n if n % 4 == 1 else -(term // n)
+            term //= x * x
+            n += 2
+        return total
+
+    two_pi = 8 * (4 * arctan_of_inverse(5) - arctan_of_inverse(239))
+    num, den = float(freq).as_integer_ratio()
+    return ((2 * num * one << 64) // (den * two_pi) + 1) // 2 % 2 ** 64
+
+
+@pytest.mark.parametrize("freq", [1.0, 10.0, 100.0, 30000.3, 65536.0, 65535.99999999999, 2 * np.pi, -3.7, -65536.0, 0.123, 1e-6, 2.0 ** -70,
+                                  -2.0 ** -63, 1e-300, 5e-324, 0.0])
+def test_turns_of_a_frequency(freq):
+    """The table's 64-bit turns per position are the nearest: 2^31 positions are off by 2^-34 of a turn, whatever the frequency."""
+    f = dn.lib["_ZN2dn9rope_turnEd"]
+    f.argtypes, f.restype = [C.c_double], C.c_uint64
+    off = (f(freq) - turns(freq)) % 2 ** 64
+    assert min(off, 2 ** 64 - off) <= 1
