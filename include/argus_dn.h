@@ -430,7 +430,8 @@ dn_status dn_op_rope(int32_t dtype, const void* x, int64_t ldx, void* y, int64_t
                      int32_t head_dim, const dn_rotation* rot, void* stream);
 
 /* RMS norm of every query and key head, then the rotation, in one pass:
- *   y = rotate(x / sqrt(mean(x^2) + eps) * gain)   (mean over the head_dim values; fp32 inside, one rounding)
+ *   y = rotate(x / sqrt(mean(x^2) + eps) * gain)   (mean over the head_dim values; fp32 inside, one rounding;
+ *                                                   finite values of any size)
  * for the `heads` heads of q [T][ldq] with q_gain and the `kv_heads` heads of k [T][ldk] with k_gain (fp32
  * [head_dim]), to q_out [T][ldqo] and k_out. v [T][ldv] (or NULL, with v_out NULL) is copied to v_out.
  * seqs NULL: row t of k (v) goes to row t of k_out (v_out); outputs may be their inputs.

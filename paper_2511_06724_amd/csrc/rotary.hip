@@ -75,6 +75,13 @@ template <int G> __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+// Maximum over the lanes of a group, in every lane.
+template <int G> __device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = 1; o < G; o *= 2) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
 template <typename T, int G, bool HALVES, bool NORM, int HC>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int chunks, int width) {
   typedef typename Quad<T>::raw raw;
@@ -157,7 +164,28 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
 #pragma unroll
           for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], ss);
           ss = group_sum<G>(lane_in ? ss : 0.f);
-          const float r = 1.f / sqrtf(ss / p.D + p.eps);
+          float mean = ss / p.D + p.eps;
+          // Squares of large or tiny values leave 32 bits (past 1.8e19; below 1e-23 where eps is no larger): the head, and the
+          // root of eps with it, is brought to one by a power of two first. A group takes one side; the usual one does not pay
+          // (48 tokens 3.64 us, without 3.60; 32,760 tokens no difference), but it would for a root here or a second look at
+          // the heads behind the loop, which keep more registers (3.69, and 137 us for 124).
+          const bool odd = !(mean >= 0x1p-80f && mean <= 0x1p120f);
+          if (__builtin_expect(__any(odd), 0)) if (odd) {
+            float top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+            // (the exponent of an infinity or of zero is 0)
+            const int root = p.eps > 0.f ? (__builtin_amdgcn_frexp_expf(p.eps) + 1) >> 1 : -1000;
+            const int down = max(__builtin_amdgcn_frexp_expf(group_max<G>(lane_in ? top : 0.f)), root);
+            ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              v[e] = ldexpf(v[e], -down);
+              ss = fmaf(v[e], v[e], ss);
+            }
+            mean = group_sum<G>(lane_in ? ss : 0.f) / p.D + ldexpf(p.eps, -2 * down);
+          }
+          const float r = 1.f / sqrtf(mean);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = v[e] * r * (hk < 0 ? gq[e] : gk[e]);
         }

@@ -169,6 +169,36 @@ def test_qk_norm_rope(dtype, pairing, dim, axes, per_axis):
         assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(v, before[:, hq + hk:])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [8, 64, 128, 200])
+def test_norm_of_large_and_tiny_heads(dtype, dim):
+    """Heads whose squares leave 32 bits, up to the largest and down to the smallest values of a type: scaling by powers of two
+    is exact, so the bound is the same."""
+    rng = np.random.default_rng(dim)
+    axes, rows = (8,), 9
+    table, freqs = dn.rope_table(axes), dn.rope_freqs(axes)
+    gain = torch.from_numpy(rng.normal(1, 0.3, dim).astype(np.float32)).to(DEV)
+    pos, pv = positions(rng, rows, 1)
+    for size in (1e38, 1e25, 3e19, 1e18, 1.0, 1e-11, 1e-13, 1e-18, 1e-25, 1e-36) + ((3e-43,) if dtype == dn.DN_FP32 else ()):
+        x = torch.from_numpy((rng.uniform(0.5, 3, (rows, 3, dim)) * rng.choice([-1, 1], (rows, 3, dim)) * size).astype(np.float32)).to(DEV)
+        x[0] = 0
+        x[0, :, dim // 2] = size                         # one value alone
+        x[1, :, 1::2] = 1e-3                             # sizes of many kinds
+        x = x.to(tdtype(dtype))
+        for eps in (0.0, 1e-40, 1e-22, 1e-6, 1e30, 3e38):
+            announce(f"norm {dtype} {dim} {size} {eps}")
+            q, k = torch.empty_like(x[:, :2]), torch.empty_like(x[:, 2:])
+            dn.op_qk_norm_rope(x[:, :2], x[:, 2:], gain, gain, eps, pos, table, q, k)
+            ref, tol = norm_rope_ref(host(x), host(gain), float(np.float32(eps)), pv, freqs, axes, P.PAIRS, dtype)
+            close(host(torch.cat([q, k], 1)), ref, tol + 2.0 ** -130)    # (an output below 2^-126 has fewer bits)
+    # infinities and NaN as the formula has them
+    x = torch.ones(2, 1, dim, device=DEV, dtype=tdtype(dtype))
+    x[0, 0, 3], x[1, 0, 5] = float("inf"), float("nan")
+    q, k, zero = torch.empty_like(x), torch.empty_like(x), torch.zeros(2, 1, device=DEV, dtype=torch.int32)
+    dn.op_qk_norm_rope(x, x, gain, gain, 1e-6, zero, dn.rope_table((2,)), q, k)
+    assert torch.isnan(q[0, 0, 3]) and (q[0, 0, 4:] == 0).all() and torch.isnan(q[1]).all()
+
+
 def cache_rows(q_len, kv_start, kv_len):
     return [kv_start[s] + kv_len[s] - n + i for s, n in enumerate(q_len) for i in range(n)]
 
