@@ -451,7 +451,7 @@ dn_status dn_op_qk_norm_rope(int32_t dtype, const void* q, int64_t ldq, const vo
  * zeros. Keys a row does not see carry no weight, infinities and NaN among them too (a call that meets such values
  * may round its sums in another order). Softmax and sums
  * fp32; bf16 probabilities enter the product rounded to bf16. |scale| <= 1e38.
- * T * (heads / kv_heads) < 2^31 - 65536.
+ * T * (heads / kv_heads) < 2^31 - 65536. Sequences of 2^31 - 65536 keys or more are skipped like those outside the tensors.
  * ws: device, 16-byte aligned, dn_attention_packed_bytes bytes (0: NULL) for the same T, heads, n and
  * max_kv_len, contents arbitrary, free when the call's work has finished; overlapping calls need workspaces of
  * their own. */

@@ -76,7 +76,7 @@ template <int BM> __device__ __forceinline__ bool find_unit(const PackedAttnPara
     u.len_k = __builtin_amdgcn_readfirstlane(p.seqs.kv_len[s]);
     u.k0 = from_lane(p.seqs.kv_start[s], 0);
   }
-  if (a < 0 || b <= a || b > p.T || u.len_k < 0 || u.k0 < 0 || u.k0 > p.kv_rows - u.len_k) return false;
+  if (!sequence_attends(a, b, p.T, u.len_k, u.k0, p.kv_rows)) return false;
   u.q0 = a;
   u.len_q = b - a;
   const long long rows = (long long)u.len_q * group, row0 = (slot - place(a, s)) * BM;
@@ -88,7 +88,7 @@ template <int BM> __device__ __forceinline__ bool find_unit(const PackedAttnPara
 
 // Keys a token of the unit's sequence sees.
 __device__ __forceinline__ int limit(const PackedAttnParams& p, const Unit& u, int token) {
-  return p.causal ? max(0, token + u.len_k - u.len_q + 1) : u.len_k;
+  return p.causal ? max(0, token + 1 + (u.len_k - u.len_q)) : u.len_k;
 }
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
@@ -794,7 +794,7 @@ struct Walk {
     if (i < p.seqs.n) {
       qa = p.seqs.q_start[i], qb = p.seqs.q_start[i + 1], len = p.seqs.kv_len[i];
       k0 = p.seqs.kv_start[i];
-      if (qa >= 0 && qb > qa && qb <= p.T && len >= 0 && k0 >= 0 && k0 <= p.kv_rows - len)
+      if (sequence_attends(qa, qb, p.T, len, k0, p.kv_rows))
         cost = ((long long)(qb - qa) * group + 31) / 32 * key_blocks(len);
     }
     incl = cost;

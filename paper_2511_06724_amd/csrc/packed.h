@@ -18,6 +18,13 @@ struct Sequences {
   const int* kv_len = nullptr;          // [n]
 };
 
+// Whether attention takes a sequence: packed rows [a, b) of T, `len` keys from k0 of kv_rows. Key positions, a tile past the last
+// one among them, are counted in 32 bits.
+constexpr int kMaxKeys = 0x7fffffff - 65536;
+__host__ __device__ __forceinline__ bool sequence_attends(int a, int b, long long T, int len, long long k0, long long kv_rows) {
+  return a >= 0 && b > a && b <= T && len >= 0 && len <= kMaxKeys && k0 >= 0 && k0 <= kv_rows - len;
+}
+
 // Largest s in [0, n) with first(s) <= x for a non-decreasing first, or -1, by the G lanes of a lane
 // group (G a power of two, the group's lanes converged): every step probes G places, so up to 64
 // sequences take one or two dependent loads. It ends, in bounds, for any values of `first`.

@@ -528,6 +528,27 @@ def test_offsets_past_32_bits(dtype):
     assert torch.equal(k[-3:], ko) and torch.equal(v[-3:], x)
 
 
+def test_the_longest_keys():
+    """As many keys as are counted, equal scores: first, middle and last ones have their weights. More are skipped."""
+    torch.cuda.empty_cache()
+    rows, most = 2 ** 31 - 1, 2 ** 31 - 65537
+    if torch.cuda.mem_get_info()[0] < rows * 64 + 2 ** 30:
+        pytest.skip("137 GB of keys")
+    kv = torch.zeros(rows, 1, 32, device=DEV, dtype=torch.bfloat16)
+    kv[0], kv[2 ** 30 + 5], kv[most - 1] = 1.0, 2.0, 4.0
+    kv[most:] = 8.0
+    q = torch.zeros(3, 1, 32, device=DEV, dtype=torch.bfloat16)
+    for causal in (True, False):
+        o = torch.full_like(q, 7.0)
+        seqs = dn.Sequences(int_t([0, 1, 2, 3]), int_t([0, 0, most - 1], torch.int64), int_t([most, rows, 2]), most)
+        dn.op_attention_packed(q, kv, kv, o, seqs, causal=causal, ws=workspace(q, kv, seqs))
+        got = host(o)
+        # parts of 2^21 keys or so are exact, their sum rounds 1024 times
+        assert (np.abs(got[0] * most / 7 - 1) <= U[dn.DN_BF16] + 1030 * W).all() and (got[1] == 7).all() and (got[2] == 6).all()
+    del kv
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.0])
 def test_scales(scale):
     for dtype in TYPES:

@@ -1,12 +1,15 @@
 """Argument checks of the packed-sequence entry points (no GPU: every case is refused before any device work)."""
 
 import ctypes as C
+import os
+import subprocess
 
 import numpy as np
 import pytest
 import torch
 
 from paper_2511_06724_amd import dn
+from tests.test_epilogue_cpu import HIPCC, ROOT
 
 P = 4096  # a 16-byte aligned address that is never followed
 
@@ -175,3 +178,37 @@ def test_turns_of_a_frequency(freq):
     f.argtypes, f.restype = [C.c_double], C.c_uint64
     off = (f(freq) - turns(freq)) % 2 ** 64
     assert min(off, 2 ** 64 - off) <= 1
+
+
+ATTENDS = r"""
+#include "packed.h"
+#include <cstdio>
+int main() {
+  const int most = 0x7fffffff;
+  const long long rows = 1ll << 40;
+  struct { int a, b; long long T; int len; long long k0, rows; bool want; } c[] = {
+    {0, 1, 1, 0, 0, 1, true}, {0, 1, 1, 1, 0, 1, true}, {0, 1, 1, 1, 1, 1, false}, {0, 1, 1, 2, 0, 1, false}, {1, 1, 9, 1, 0, 9, false},
+    {-1, 1, 9, 1, 0, 9, false}, {2, 1, 9, 1, 0, 9, false}, {0, 10, 9, 1, 0, 9, false}, {0, 1, 1, -1, 0, 9, false}, {0, 1, 1, 1, -1, 9, false},
+    {0, 1, 1, most - 65536, 0, rows, true}, {0, 1, 1, most - 65535, 0, rows, false}, {0, 1, 1, most, 0, rows, false},
+    {0, 1, 1, most - 65536, rows - most + 65536, rows, true}, {0, 1, 1, most - 65536, rows - most + 65537, rows, false},
+    {0, 1, 1, 5, 0x7fffffffffffffffll, rows, false}, {most - 1, most, most, 5, 0, 5, true}, {0, most, most - 1, 5, 0, 5, false}};
+  for (const auto& x : c)
+    if (dn::sequence_attends(x.a, x.b, x.T, x.len, x.k0, x.rows) != x.want)
+      return std::printf("%d %d %lld %d %lld %lld\n", x.a, x.b, x.T, x.len, x.k0, x.rows), 1;
+  // a tile past the last key is still a number of 32 bits
+  int end;
+  return __builtin_add_overflow(dn::kMaxKeys, 65536, &end);
+}
+"""
+
+
+@pytest.mark.skipif(HIPCC is None, reason="no hipcc")
+def test_sequences_that_attention_takes(tmp_path):
+    """The check of a sequence's rows and lengths, compiled for the host: inside the tensors, keys counted in 32 bits."""
+    src, exe = tmp_path / "attends.hip", tmp_path / "attends"
+    src.write_text(ATTENDS)
+    r = subprocess.run([HIPCC, "--offload-host-only", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I",
+                        os.path.join(ROOT, "paper_2511_06724_amd", "csrc"), str(src), "-o", str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, r.stdout
