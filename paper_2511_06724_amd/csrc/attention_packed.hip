@@ -92,6 +92,8 @@ __device__ __forceinline__ int limit(const PackedAttnParams& p, const Unit& u, i
 }
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+// x f; an infinity or a NaN of a value that is seen stays what it is also when its weight f has become zero beside a larger one.
+__device__ __forceinline__ float weigh(float x, float f) { return not_finite(x) ? x : x * f; }
 __device__ __forceinline__ bool is_nan(float x) { return (__float_as_uint(x) & 0x7fffffffu) > 0x7f800000u; }
 
 // Maximum of scores. (fmaxf would quiet every matrix-core result first, one operation each; this one
@@ -231,7 +233,7 @@ __device__ __forceinline__ void careful_rows(const PackedAttnParams& p, const Un
         l *= alpha;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          o[r] *= alpha;
+          o[r] = weigh(o[r], alpha);
           s[r] = to_f32(from_f32<T>(fast_exp2(s[r] - m)));
           l += s[r];
         }
@@ -1071,8 +1073,19 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D * siz
 template <int D> struct JoinedRow {
   static constexpr int E = (D + 63) / 64;
   float top = kLowest, sum = 0.f, v[E] = {};
-  // (with loads of W parts side by side)
+  // Parts first, first + step, .. of n. Again with weigh() if a value is a NaN, so that the usual sum costs no more.
   template <int W> __device__ __forceinline__ void add(const Partials& part, int w0, int n, int r, int first, int step) {
+    add_parts<W, false>(part, w0, n, r, first, step);
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) nan |= is_nan(v[e]);
+    if (__builtin_expect(__any(nan), 0)) {
+      *this = JoinedRow();
+      add_parts<1, true>(part, w0, n, r, first, step);
+    }
+  }
+  // (with loads of W parts side by side)
+  template <int W, bool WEIGH> __device__ __forceinline__ void add_parts(const Partials& part, int w0, int n, int r, int first, int step) {
     const int lane = threadIdx.x & 63;
     auto at = [&](int k) { return (2ll * (w0 + k) + (k == 0 ? 1 : 0)) * 32 + r; };
     for (int c = first; c < n; c += 64 * step) {
@@ -1093,7 +1106,7 @@ template <int D> struct JoinedRow {
       top = up;
       sum *= alpha;
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= alpha;
+      for (int e = 0; e < E; ++e) v[e] = WEIGH ? weigh(v[e], alpha) : v[e] * alpha;
       const float f = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top), fl = f * ml.y;
       for (int k0 = 0; k0 < cnt; k0 += W) {
         if (k0) load(k0);
@@ -1103,7 +1116,7 @@ template <int D> struct JoinedRow {
             const float fk = __shfl(f, k0 + j, 64);
             sum += __shfl(fl, k0 + j, 64);
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] += fk * x[j][e];
+            for (int e = 0; e < E; ++e) v[e] += WEIGH ? weigh(x[j][e], fk) : fk * x[j][e];
           }
         }
       }
@@ -1168,7 +1181,7 @@ template <typename T, int D> __global__ __launch_bounds__(64 * kJoin) void join_
         const float f = fast_exp2(s_top[k] - all.top);
         all.sum += f * s_sum[k];
 #pragma unroll
-        for (int e = 0; e < E; ++e) all.v[e] += f * s_v[k][e * 64 + lane];
+        for (int e = 0; e < E; ++e) all.v[e] += weigh(s_v[k][e * 64 + lane], f);
       }
       all.template store<T>(p, group, u, r);
     }

@@ -459,6 +459,26 @@ def test_masked_keys_have_no_influence(dtype, dim, group):
     assert np.isnan(got[100:n]).all() and (b.o[n + 40:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,m,hq,hk,dim", [(1, 100, 2, 2, 64), (1, 4000, 2, 2, 64), (1, 60000, 1, 1, 64), (130, 3000, 8, 1, 128),
+                                           (300, 700, 2, 2, 128), (40, 90, 3, 3, 32), (1, 9000, 8, 1, 96)])
+@pytest.mark.parametrize("first", [True, False])
+def test_an_infinite_value_of_little_weight(dtype, n, m, hq, hk, dim, first):
+    """Its weight is e^-300 of the sum, zero in 32 bits: the row's value is infinite all the same, wherever the key lies."""
+    b = Batch([n], [m], hq, hk, dim, dtype)
+    b.q.zero_()
+    b.q[..., 0] = 1.0
+    a, last = b.start[0], b.start[0] + m - n
+    low, high = (a + 1, last) if first else (last, a + 1)
+    b.k[a:a + m, :, 0] = 0.0
+    b.k[high, :, 0] = 300.0
+    b.v[low, :, 3], b.v[low, :, 5], b.v[low, :, 7] = float("inf"), -float("inf"), float("nan")
+    got = host(b.run(True, scale=1.0))[:n]
+    want = host(b.v[high]).repeat(hq // hk, 0)
+    assert (got[..., 3] == np.inf).all() and (got[..., 5] == -np.inf).all() and np.isnan(got[..., 7]).all()
+    assert np.array_equal(got[..., 8:], np.broadcast_to(want[:, 8:], got[..., 8:].shape))
+
+
 def test_extreme_scores():
     """Scores of +-1e30 and equal ones at the lowest finite value: the largest take all, no NaN."""
     b = Batch([4], [70], 1, 1, 64, dn.DN_FP32)
