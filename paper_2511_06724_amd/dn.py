@@ -185,6 +185,16 @@ def _stream(stream):
     return getattr(stream, "cuda_stream", stream)
 
 
+def _new(shape, dtype, device, stream):
+    """A new tensor for a call on `stream` (None: the current one), of the memory that is free in that stream's order: of the
+    current stream's, work that is still to come there may hold it."""
+    import torch
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, device=device, dtype=dtype)
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device)):
+        return torch.empty(shape, device=device, dtype=dtype)
+
+
 @functools.lru_cache(maxsize=None)
 def _current_device():
     import torch
@@ -474,7 +484,7 @@ def mx_quantize(dtype, x, q=None, stream=None):
     xt, ldx, rows, cols = _rows(x, "mx_quantize")
     need = mx_bytes(dtype, rows, cols)
     if q is None:
-        q = torch.empty(need, device=x.device, dtype=torch.uint8)
+        q = _new(need, torch.uint8, x.device, stream)
     _buffer(q, need, "mx_quantize")
     _check(lib.dn_mx_quantize(dtype, xt, _ptr(x), ldx, rows, cols, _ptr(q), _stream(stream)))
     return q
@@ -485,7 +495,7 @@ def mx_dequantize(dtype, q, rows, cols, y=None, stream=None):
     import torch
     _buffer(q, mx_bytes(dtype, rows, cols), "mx_dequantize")
     if y is None:
-        y = torch.empty(rows, cols, device=q.device, dtype=torch.float32)
+        y = _new((rows, cols), torch.float32, q.device, stream)
     yt, ldy, r, c = _rows(y, "mx_dequantize")
     if yt != DN_FP32 or (r, c) != (rows, cols):
         raise ValueError("mx_dequantize: y must be float32 [rows, cols]")
@@ -595,7 +605,7 @@ def _dense(t, dtype, shape, name):
 
 class Sequences:
     """The sequences of a packed batch: q_start int32 [n + 1], kv_start int64 [n], kv_len int32 [n] (CUDA tensors, read
-    when the work runs), and a bound of kv_len the caller knows."""
+    when the work runs; kept until then), and a bound of kv_len the caller knows."""
 
     def __init__(self, q_start, kv_start, kv_len, max_kv_len):
         import torch
@@ -623,7 +633,8 @@ def rope_freqs(axis_dims, theta=10000.0, per_axis=True):
 
 
 class RopeTable:
-    """A rotation table on the GPU (dn_rope_table)."""
+    """A rotation table on the GPU (dn_rope_table), filled on `stream`: calls on other streams come after that, and it is kept
+    until they have finished."""
 
     def __init__(self, axis_dims, freqs, device, stream=None):
         import torch
@@ -633,7 +644,7 @@ class RopeTable:
         if dims.ndim != 1 or f.shape != (sum(self.axis_dims) // 2,):
             raise ValueError("rope_table: one frequency per rotated pair is needed")
         self.rot_dim, self.n_axes = sum(self.axis_dims), len(self.axis_dims)
-        self.data = torch.empty(DN_ROPE_TABLE_BYTES, device=device, dtype=torch.uint8)
+        self.data = _new(DN_ROPE_TABLE_BYTES, torch.uint8, torch.device(device), stream)
         self.address, self.device = self.data.data_ptr(), self.data.get_device()
         _check(lib.dn_rope_table(f.ctypes.data, dims.ctypes.data, self.n_axes, self.address,
                                  _stream_on(self.device, stream, "rope_table")))
@@ -658,8 +669,7 @@ def op_rope(x, pos, table, y=None, pairing=DN_ROPE_PAIRS, stream=None):
     """Rotates the heads of x [rows, heads, head_dim] to pos int32 [rows, axes] (into y, a new tensor, or x itself)."""
     src, ldx, dt, shape = _heads(x, "op_rope")
     if y is None:
-        import torch
-        y = torch.empty(shape, device=x.device, dtype=x.dtype)
+        y = _new(shape, x.dtype, x.device, stream)
     dst, ldy, yt, y_shape = _heads(y, "op_rope: y")
     if yt != dt or y_shape != shape:
         raise ValueError("op_rope: y must have the type and shape of x")
@@ -753,8 +763,7 @@ def pack_weight(dtype, w, N, K, stream=None):
     """Row-major device weight [N][K] (dtype elements; fp32 for DN_FP8 and DN_MXFP4) -> a new tensor in
     the GEMM's packed layout (uint8 for those two: codes, then the scales)."""
     import torch
-    out = torch.empty(packed_weight_elems(dtype, N, K), device=w.device,
-                      dtype=torch.uint8 if dtype in (DN_FP8, DN_MXFP4) else w.dtype)
+    out = _new(packed_weight_elems(dtype, N, K), torch.uint8 if dtype in (DN_FP8, DN_MXFP4) else w.dtype, w.device, stream)
     _check(lib.dn_pack_weight(dtype, _ptr(w), N, K, _ptr(out), _stream(stream)))
     return out
 

@@ -660,6 +660,36 @@ def test_tensors_of_another_device_are_refused():
         dn.op_rope(b.q, torch.zeros(len(b.q), 1, dtype=torch.int32), dn.rope_table((64,)))
 
 
+@pytest.mark.parametrize("raw", [False, True])
+def test_new_tensors_of_a_call_on_another_stream(raw):
+    """Their memory is not what the current stream has freed and still writes."""
+    other = torch.cuda.Stream()
+    on = other.cuda_stream if raw else other
+    x, _ = heads(np.random.default_rng(0), 4096, 8, 64, dn.DN_FP32)
+    m = x.reshape(4096, 512)
+    pos, w = torch.arange(4096, device=DEV, dtype=torch.int32)[:, None].contiguous(), torch.randn(512, 1024, device=DEV)
+    table = dn.rope_table((64,))
+    want = dn.op_rope(x, pos, table)
+    q = dn.mx_quantize(dn.DN_MXFP8, m)
+    deq, packed = dn.mx_dequantize(dn.DN_MXFP8, q, 4096, 512), dn.pack_weight(dn.DN_FP32, w, 512, 1024)
+    busy = torch.randn(8192, 8192, device=DEV)
+    calls = [(want, lambda: dn.op_rope(x, pos, table, stream=on)), (table.data, lambda: dn.rope_table((64,), stream=on).data),
+             (q, lambda: dn.mx_quantize(dn.DN_MXFP8, m, stream=on)), (packed, lambda: dn.pack_weight(dn.DN_FP32, w, 512, 1024, stream=on)),
+             (deq, lambda: dn.mx_dequantize(dn.DN_MXFP8, q, 4096, 512, stream=on))]
+    for expect, call in calls:
+        torch.cuda.synchronize()
+        for _ in range(4):
+            torch.mm(busy, busy)                        # some milliseconds
+        freed = torch.empty_like(expect)
+        freed.fill_(3)
+        del freed
+        got = call()
+        other.synchronize()
+        torch.cuda.synchronize()
+        n = 4096 * (512 + 16) if expect is q else None      # (what follows the scales is never written)
+        assert torch.equal(got[:n], expect[:n])
+
+
 def test_two_streams_at_once():
     bs = [Batch([1, 3], [2500, 1200], 8, 2, 128, dn.DN_BF16, seed=s) for s in (1, 2)]
     want = [b.run(True).clone() for b in bs]
