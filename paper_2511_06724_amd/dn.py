@@ -593,8 +593,8 @@ def _heads(x, name):
     dt = _head_types().get(x.dtype)
     if dt is None:
         raise ValueError(f"{name}: heads must be float32 or bfloat16")
-    ld = stride[0]
-    return x.data_ptr(), shape[1] * dim if shape[0] == 1 and ld < shape[1] * dim else ld, dt, shape
+    # the stride of a single row (one token of a long projection) says nothing
+    return x.data_ptr(), shape[1] * dim if shape[0] == 1 else stride[0], dt, shape
 
 
 def _dense(t, dtype, shape, name):

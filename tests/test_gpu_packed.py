@@ -660,6 +660,22 @@ def test_tensors_of_another_device_are_refused():
         dn.op_rope(b.q, torch.zeros(len(b.q), 1, dtype=torch.int32), dn.rope_table((64,)))
 
 
+def test_the_last_token_of_a_long_projection():
+    """One row whose stride is more than rows may lie apart, and no multiple of 16 bytes."""
+    width, rows = 3 * 4 * 64 + 1, 11000
+    whole = torch.randn(1, rows, width, device=DEV).to(torch.bfloat16)
+    at = (rows - 1) * width // 8 * 8                   # 16-byte aligned
+    x = whole.flatten()[at:][:768].view(12, 64).as_strided((1, 12, 64), (rows * width, 64, 1))
+    q, k, v = x[:, :4], x[:, 4:8], x[:, 8:]
+    assert q.stride(0) > 2 ** 23
+    pos, gain, table = int_t([[rows]]), torch.ones(64, device=DEV), dn.rope_table((64,))
+    qo, ko, vo, qc, kc, vc = (torch.empty(1, 4, 64, device=DEV, dtype=x.dtype) for _ in range(6))
+    dn.op_qk_norm_rope(q, k, gain, gain, 1e-6, pos, table, qo, ko, v, vo)
+    dn.op_qk_norm_rope(q.contiguous(), k.contiguous(), gain, gain, 1e-6, pos, table, qc, kc, v.contiguous(), vc)
+    assert torch.equal(qo, qc) and torch.equal(ko, kc) and torch.equal(vo, vc) and torch.equal(v, vo)
+    assert torch.equal(dn.op_rope(q, pos, table), dn.op_rope(q.contiguous(), pos, table))
+
+
 @pytest.mark.parametrize("raw", [False, True])
 def test_new_tensors_of_a_call_on_another_stream(raw):
     """Their memory is not what the current stream has freed and still writes."""

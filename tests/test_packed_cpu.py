@@ -146,6 +146,13 @@ def test_binding_refuses_host_tensors():
             call()
 
 
+@pytest.mark.parametrize("stride", [0, 3, 100, 256, 2 ** 24, 2 ** 40])
+def test_a_single_row_has_any_stride(stride):
+    x = t(256).as_strided((1, 4, 64), (stride, 64, 1))
+    assert dn._heads(x, "x")[1] == 256
+    assert dn._heads(t(512).as_strided((2, 4, 64), (256, 64, 1)), "x")[1] == 256
+
+
 def test_default_frequencies():
     assert dn.rope_freqs((4, 4), 100.0) == [1.0, 0.1, 1.0, 0.1]
     assert np.allclose(dn.rope_freqs((4, 4), 100.0, per_axis=False), 100.0 ** (-np.arange(4) / 4))
