@@ -1203,8 +1203,9 @@ size_t partials(void* ws, int D, int shares, Partials& r) {
   return n;
 }
 
-// Divided calls: one wave a workgroup, up to 1024 of them (four a CU, by their rings): 32 contexts up to 54 k, 32/8 heads of
-// 128: 181 us, with two waves and 512 200, with four and 256 212. Others: four waves on a unit.
+// Divided calls: one wave a workgroup, up to 1024 of them: 32 contexts up to 54 k, 32/8 heads of 128: 181 us, with two waves and
+// 512 200, with four and 256 212. Their LDS lets four run on a CU at once, but of wide fp32 heads fewer (96: three, 128: two, by
+// careful_rows' tiles): the last of those shares start as others end.
 constexpr int most_shares(int row_bytes) { return row_bytes <= 64 ? 2048 : 1024; }
 
 // Of few blocks the shares are fewer: with a block's time t and a part's time in the join c, s shares of B blocks, of which the
@@ -1216,28 +1217,22 @@ int shares_of(long long blocks, long long most, long long units, int elem, int D
   return (int)std::min<long long>({std::max((long long)std::min(s, 1e9), units), blocks, most_shares(D * elem)});
 }
 
-template <typename T, int D> void launch_narrow(const PackedAttnParams& p, int shares, hipStream_t s) {
+// Rows of a unit, in the mean.
+int rows_of_unit(long long rows, int n) { return (int)std::min<long long>(32, (rows + n - 1) / n); }
+
+template <typename T, int D> void launch_narrow(const PackedAttnParams& p, const PackedPlan& plan, hipStream_t s) {
   constexpr int R = D * sizeof(T) <= 128 ? 4 : 2;
   const long long group = p.heads / p.kv_heads, rows = p.T * group;
   Partials part;
-  if (shares) {
-    partials(p.ws, D, shares, part);
-    // the tensors' rows bound the blocks, too
-    const long long blocks = (p.kv_rows / 32 + p.seqs.n) * p.kv_heads * ((rows + 32ll * p.seqs.n - 1) / (32ll * p.seqs.n));
-    const long long most = std::min(blocks, (p.max_kv + 31ll) / 32);
-    shares = std::min(shares, shares_of(blocks, most, (rows / 32 + p.seqs.n) * p.kv_heads, sizeof(T), D));
+  if (plan.most) {
+    const int shares = plan.shares;
+    partials(p.ws, D, plan.most, part);
     hipLaunchKernelGGL((packed_narrow_kernel<T, D, 1, R, true>), dim3(shares), dim3(64), 0, s, p, (int)group, shares, part);
     DN_HIP(hipGetLastError());
-    const long long per = std::min<long long>(32, (rows + p.seqs.n - 1) / p.seqs.n);  // rows of a unit, in the mean
-    const long long units = (rows / 32 + p.seqs.n) * p.kv_heads;
-    // up to about 32 parts of the largest unit, and not so few rows that every one can have a workgroup (16/2 x 128, 128 tokens
-    // behind 16 k keys: 71 us, with a workgroup per row 128; 13 single tokens, 1/1 x 96: 14.8 and 10.4). The rows of few
-    // units go over several workgroups, a row or so a wave (the former: 98 with one)
-    if (shares * per > 1024 && shares * most <= 32 * blocks) {
-      const unsigned split = (unsigned)std::max<long long>(1, std::min(per / 4, 1024 / units));
-      hipLaunchKernelGGL((join_rows_kernel<T, D>), dim3((shares + 3) / 4, split), dim3(256), 0, s, p, (int)group, shares, part);
+    if (plan.join == kJoinRows) {
+      hipLaunchKernelGGL((join_rows_kernel<T, D>), dim3((shares + 3) / 4, plan.split), dim3(256), 0, s, p, (int)group, shares, part);
     } else {
-      hipLaunchKernelGGL((join_kernel<T, D>), dim3(shares, (unsigned)per), dim3(64 * kJoin), 0, s, p, (int)group, part);
+      hipLaunchKernelGGL((join_kernel<T, D>), dim3(shares, rows_of_unit(rows, p.seqs.n)), dim3(64 * kJoin), 0, s, p, (int)group, part);
     }
   } else {
     constexpr int NW = D * sizeof(T) > 256 ? 2 : 4;
@@ -1260,15 +1255,6 @@ template <int D> void launch_f32(const PackedAttnParams& p, hipStream_t s) {
 
 bool attention_packed_dim(int D) { return D == 32 || D == 64 || D == 96 || D == 128; }
 
-namespace {
-
-// How a call is run. A function of sizes alone (of the 256 CUs of the one GPU this is built for), so that the workspace does
-// not depend on the device at hand.
-struct Plan {
-  bool narrow = false;  // 32 rows a unit; else whole tiles of rows
-  int shares = 0;       // most workgroups over all key blocks (0: one per unit)
-  int waves = 0;        // of 32 rows, of a tile (bf16)
-};
 // Measured, us (heads/kv_heads x head dim):
 //  - few rows a sequence: narrow. Up to 256 keys a unit is one workgroup's (77 keys, 20/20 x 64: 6.1); longer ones are divided.
 //  - too few tiles to fill the CUs and long keys: narrow, divided. A tile's time goes with the keys (0.017 us each of 128
@@ -1283,29 +1269,41 @@ struct Plan {
 //  - tiles: 8 waves of 32 rows where there are tiles for every CU and the border is small beside them (20/20 x 128, two
 //    images of 4173 tokens: 357, 4 waves 402; 8 x 512 tokens: 40.0, 36.3); 2 waves for short prompts (20/20 x 64,
 //    64 of 49 tokens in the mean: 18.1, 4 waves 20.6, 8 waves 39.2); else 4 (64 wide: 2 x 10/10, 4096 tokens: 120, 8 waves 141).
-Plan plan(int elem, int D, long long T, int heads, int kv_heads, int n, int max_kv) {
+PackedPlan attention_packed_plan(int elem, int D, long long T, int heads, int kv_heads, int n, int max_kv, long long kv_rows) {
   const long long group = heads / kv_heads, rows = T * group, units = (rows / 32 + n) * kv_heads;
   auto tiles = [&](int bm) { return (rows / bm + n) * kv_heads; };
   const bool few = rows <= 32ll * n, some = rows < 96ll * n;
-  Plan r;
-  r.narrow = few || (elem == 4 ? some || tiles(128) < 128 : tiles(128) <= (rows < 1024ll * n ? 112 : 64) - 100000 / max_kv);
-  if (r.narrow) {
-    if (max_kv > (few || elem == 2 || D > 64 ? 256 : 1024)) r.shares = (int)std::min<long long>(most_shares(D * elem), units * ((max_kv + 31ll) / 32));
-  } else {
-    r.waves = some ? 2 : D == 128 && rows >= 1024ll * n && tiles(256) >= 256 ? 8 : 4;
+  PackedPlan r;
+  if (!(few || (elem == 4 ? some || tiles(128) < 128 : tiles(128) <= (rows < 1024ll * n ? 112 : 64) - 100000 / max_kv))) {
+    r.waves = elem == 4 ? 4 : some ? 2 : D == 128 && rows >= 1024ll * n && tiles(256) >= 256 ? 8 : D == 96 ? 6 : 4;
+    return r;
   }
+  if (max_kv <= (few || elem == 2 || D > 64 ? 256 : 1024)) return r;
+  r.most = (int)std::min<long long>(most_shares(D * elem), units * ((max_kv + 31ll) / 32));
+  // the tensors' rows bound the blocks, too
+  const long long blocks = (kv_rows / 32 + n) * kv_heads * ((rows + 32ll * n - 1) / (32ll * n));
+  const long long longest = std::min(blocks, (max_kv + 31ll) / 32);
+  r.shares = std::min(r.most, shares_of(blocks, longest, units, elem, D));
+  // rows' joining: up to about 32 parts of the largest unit, and not so few rows that every one can have a workgroup (16/2 x
+  // 128, 128 tokens behind 16 k keys: 71 us, with a workgroup per row 128; 13 single tokens, 1/1 x 96: 14.8 and 10.4). The rows
+  // of few units go over several workgroups, a row or so a wave (the former: 98 with one)
+  const long long per = rows_of_unit(rows, n);
+  r.join = r.shares * per > 1024 && r.shares * longest <= 32 * blocks ? kJoinRows : kJoinUnits;
+  if (r.join == kJoinRows) r.split = (int)std::max<long long>(1, std::min(per / 4, 1024 / units));
   return r;
 }
 
+namespace {
+
 template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) {
-  const Plan r = plan(sizeof(T), D, p.T, p.heads, p.kv_heads, p.seqs.n, p.max_kv);
-  if (r.narrow) return launch_narrow<T, D>(p, r.shares, s);
+  const PackedPlan r = attention_packed_plan(sizeof(T), D, p.T, p.heads, p.kv_heads, p.seqs.n, p.max_kv, p.kv_rows);
+  if (!r.waves) return launch_narrow<T, D>(p, r, s);
   if constexpr (sizeof(T) == 4) {
     launch_f32<D>(p, s);
   } else if constexpr (D == 128) {
     r.waves == 8 ? launch_pipe<D, 64, 8, 4, 2>(p, s) : r.waves == 4 ? launch_pipe<D, 32, 4, 5, 2>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
   } else if constexpr (D == 96) {  // (six waves: whole loads)
-    r.waves == 4 ? launch_pipe<D, 32, 6, 5, 3>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
+    r.waves == 6 ? launch_pipe<D, 32, 6, 5, 3>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
   } else if constexpr (D == 64) {
     r.waves == 4 ? launch_pipe<D, 32, 4, 5, 3>(p, s) : launch_pipe<D, 32, 2, 5, 2>(p, s);
   } else {
@@ -1316,9 +1314,9 @@ template <typename T, int D> void run(const PackedAttnParams& p, hipStream_t s) 
 }  // namespace
 
 size_t attention_packed_bytes(int elem, long long T, int heads, int kv_heads, int D, int n, int max_kv) {
-  const Plan r = plan(elem, D, T, heads, kv_heads, n, max_kv);
+  const PackedPlan r = attention_packed_plan(elem, D, T, heads, kv_heads, n, max_kv, 0);  // (of the most shares)
   Partials part;
-  return r.shares ? partials(nullptr, D, r.shares, part) : 0;
+  return r.most ? partials(nullptr, D, r.most, part) : 0;
 }
 
 template <typename T> void attention_packed(const PackedAttnParams& p, int D, hipStream_t s) {

@@ -100,6 +100,16 @@ struct PackedAttnParams {
   Sequences seqs;
 };
 bool attention_packed_dim(int D);
+// How a call is run: a function of sizes alone (of the 256 CUs of the one GPU this is built for), so that the workspace does
+// not depend on the device at hand.
+enum PackedJoin { kJoinNone, kJoinRows, kJoinUnits };
+struct PackedPlan {
+  int waves = 0;   // of 32 rows, of a tile (fp32: four); 0: units of 32 rows (narrow)
+  int most = 0;    // narrow: most workgroups over all key blocks, whatever kv_rows (0: one per unit)
+  int shares = 0;  // and those that are launched
+  int join = kJoinNone, split = 1;  // who joins a divided call's parts, workgroups of join_rows_kernel for four shares
+};
+PackedPlan attention_packed_plan(int elem, int D, long long T, int heads, int kv_heads, int n, int max_kv, long long kv_rows);
 // Workspace bytes (0: none).
 size_t attention_packed_bytes(int elem, long long T, int heads, int kv_heads, int D, int n, int max_kv);
 template <typename T> void attention_packed(const PackedAttnParams& p, int D, hipStream_t s);
