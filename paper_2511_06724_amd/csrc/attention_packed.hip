@@ -1205,7 +1205,8 @@ size_t partials(void* ws, int D, int shares, Partials& r) {
 
 // Divided calls: one wave a workgroup, up to 1024 of them: 32 contexts up to 54 k, 32/8 heads of 128: 181 us, with two waves and
 // 512 200, with four and 256 212. Their LDS lets four run on a CU at once, but of wide fp32 heads fewer (96: three, 128: two, by
-// careful_rows' tiles): the last of those shares start as others end.
+// careful_rows' tiles): the last of those shares start as others end. Undivided units have four
+// waves, of wide fp32 heads two.
 constexpr int most_shares(int row_bytes) { return row_bytes <= 64 ? 2048 : 1024; }
 
 // Of few blocks the shares are fewer: with a block's time t and a part's time in the join c, s shares of B blocks, of which the

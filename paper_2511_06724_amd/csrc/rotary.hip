@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
           float mean = ss / p.D + p.eps;
           // Squares of large or tiny values leave 32 bits (past 1.8e19; below 1e-23 where eps is no larger): the head, and the
           // root of eps with it, is brought to one by a power of two first. A group takes one side; the usual one does not pay
-          // (48 tokens 3.64 us, without 3.60; 32,760 tokens no difference), but it would for a root here or a second look at
+          // (48 tokens 3.63 us, without 3.60; 32,760 tokens no difference), but it would for a root here or a second look at
           // the heads behind the loop, which keep more registers (3.69, and 137 us for 124).
           const bool odd = !(mean >= 0x1p-80f && mean <= 0x1p120f);
           if (__builtin_expect(__any(odd), 0)) if (odd) {
@@ -175,7 +175,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
             // (the exponent of an infinity or of zero is 0)
-            const int root = p.eps > 0.f ? (__builtin_amdgcn_frexp_expf(p.eps) + 1) >> 1 : -1000;
+            float eps = p.eps;
+            asm volatile("" : "+v"(eps));  // (or its root is taken ahead of the loop, in every call)
+            const int root = eps > 0.f ? (__builtin_amdgcn_frexp_expf(eps) + 1) >> 1 : -1000;
             const int down = max(__builtin_amdgcn_frexp_expf(group_max<G>(lane_in ? top : 0.f)), root);
             ss = 0.f;
 #pragma unroll
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int ch
               v[e] = ldexpf(v[e], -down);
               ss = fmaf(v[e], v[e], ss);
             }
-            mean = group_sum<G>(lane_in ? ss : 0.f) / p.D + ldexpf(p.eps, -2 * down);
+            mean = group_sum<G>(lane_in ? ss : 0.f) / p.D + ldexpf(eps, -2 * down);
           }
           const float r = 1.f / sqrtf(mean);
 #pragma unroll
