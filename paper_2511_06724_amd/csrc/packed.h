@@ -20,9 +20,9 @@ struct Sequences {
 
 // Whether attention takes a sequence: packed rows [a, b) of T, `len` keys from k0 of kv_rows. Key positions, a tile past the last
 // one among them, are counted in 32 bits.
-constexpr int kMaxKeys = 0x7fffffff - 65536;
+constexpr unsigned kMaxKeys = 0x7fffffff - 65536;
 __host__ __device__ __forceinline__ bool sequence_attends(int a, int b, long long T, int len, long long k0, long long kv_rows) {
-  return a >= 0 && b > a && b <= T && len >= 0 && len <= kMaxKeys && k0 >= 0 && k0 <= kv_rows - len;
+  return a >= 0 && b > a && b <= T && static_cast<unsigned>(len) <= kMaxKeys && k0 >= 0 && k0 <= kv_rows - len;
 }
 
 // Largest s in [0, n) with first(s) <= x for a non-decreasing first, or -1, by the G lanes of a lane
